@@ -413,6 +413,174 @@ sq_status sq_prepare_weights_variant(const void *W, int32_t K, int32_t N, int64_
                                      void *stream);
 
 /*
+ * sq_quantize_grouped -- the quantizer of Sec. 3.2 with a step per group of
+ * neighbouring channels instead of one per row, and the step kept in fp16:
+ *
+ *   step[t, g] = fp16( max_{k in g} |X[t, k]| / 7 )    (1 where that rounds to 0)
+ *   code[t, k] = clamp( floor(X[t, k] / step[t, g] + 1/2), -8, 7 )
+ *
+ * For weights: transpose, rotate (sq_rotate_fp16 on the rows of W^T), then this
+ * call gives the operands of sq_w4a16_gemm_grouped.
+ *   X        device, fp16 [T, ldx]; rows 16-byte aligned (ldx % 8 == 0), ldx >= K
+ *   group    32, 64, 128 or 256; K % group == 0, K <= 131072
+ *   Q        device out, uint8 [T, K/2], 16-byte aligned; nibbles as everywhere
+ *   steps    device out, fp16 [T, K / group]
+ * T == 0 is legal and enqueues nothing.
+ */
+sq_status sq_quantize_grouped(const void *X, int64_t T, int32_t K, int64_t ldx,
+                              int32_t group, uint8_t *Q, void *steps, void *stream);
+
+/*
+ * sq_w4a16_gemm_grouped -- sq_w4a16_gemm with a step per group of K:
+ *
+ *   Y[t, n] = fp16( sum_g steps[n, g] * sum_{k in g} X[t, k] * Qw[n, k] )
+ *
+ *   X        device, fp16 [T, ldx]; rows 16-byte aligned (ldx % 8 == 0), ldx >= K
+ *   Qw       device, uint8 [N, K/2], 16-byte aligned
+ *   steps    device, fp16 [N, K / group], group 32, 64, 128 or 256
+ *   Y        device out, fp16 [T, ldy], ldy >= N
+ * Requires K % 64 == 0, K % group == 0, K <= 131072, T <= 2^24.  T == 0 or N == 0
+ * is legal and enqueues nothing.
+ */
+sq_status sq_w4a16_gemm_grouped(const void *X, int64_t T, int32_t K, int64_t ldx,
+                                const uint8_t *Qw, const void *steps, int32_t group, int32_t N,
+                                void *Y, int64_t ldy, void *stream);
+
+/*
+ * sq_rotary_table / sq_rotary_fp16 -- rotary positions on the heads of a
+ * projection's output.  Pair i of a head turns by the angle position * f_i:
+ *
+ *   (a, b)  ->  magnitude * (a cos - b sin,  b cos + a sin)
+ *
+ * with (a, b) the channels (2i, 2i + 1), or, half = 1, (i, i + rot / 2), for the
+ * first `rot` channels of a head; the others are copied as they are.
+ *
+ * sq_rotary_table   the frequencies, host only: turns[i] = f_i / (2 pi) in units of
+ *              2^-64 of a turn, rounded to nearest.  A program may write a table of
+ *              its own; the angle is then exact modulo a turn for any position.
+ *              Plain: f_i = base^(-2i / rot).  For contexts `factor` times longer
+ *              than the `trained` positions:
+ *                SQ_ROTARY_LINEAR   f_i / factor
+ *                SQ_ROTARY_BASE     base times factor^(rot / (rot - 2)); rot > 2
+ *                SQ_ROTARY_PARTS    pairs that make more than `high` turns over the
+ *                    trained positions keep f_i, those below `low` turns take
+ *                    f_i / factor, between them the share of f_i rises linearly
+ *                    with the turns
+ *   rot        even, 2 .. SQ_ROTARY_MAX_CHANNELS; base in (1, 1e18]
+ *   factor     in [1, 1e9], for the three scaled kinds; trained > 0 and
+ *              0 <= low < high for SQ_ROTARY_PARTS; unused ones are not read
+ *   turns      host out, uint64 [rot / 2]
+ *
+ * sq_rotary_fp16
+ *   X, Y       device, fp16; head h of token t begins at t * ldx + h * ldh (Y: ldy,
+ *              ldyh) and has D channels; ldh >= D, ldx >= (H - 1) ldh + D.  Y may be
+ *              X with the same strides (in place: the channels behind `rot` are not
+ *              touched); any other overlap is an error of the caller.  Multiples of
+ *              8 for D and the strides, 16 for rot, and 16-byte aligned pointers make
+ *              it fast; nothing but 2-byte alignment is required.
+ *   positions  device, int32 [T], any value
+ *   turns      device, uint64 [rot / 2]
+ *   rot        even, 0 .. D; half 0 or 1; magnitude: 1 unless the scaling asks for
+ *              another (it multiplies cosine and sine)
+ * Sums in fp32, angles within 2^-25 of a turn, one rounding to fp16.  T == 0 or
+ * H == 0 is legal and enqueues nothing.
+ */
+#define SQ_ROTARY_MAX_CHANNELS 1024
+typedef enum {
+    SQ_ROTARY_PLAIN = 0,
+    SQ_ROTARY_LINEAR = 1,
+    SQ_ROTARY_BASE = 2,
+    SQ_ROTARY_PARTS = 3
+} sq_rotary_scaling;
+sq_status sq_rotary_table(int32_t rot, double base, sq_rotary_scaling scaling, double factor,
+                          double trained, double low, double high, uint64_t *turns);
+sq_status sq_rotary_fp16(const void *X, int64_t T, int32_t H, int32_t D, int64_t ldx, int64_t ldh,
+                         const int32_t *positions, const uint64_t *turns, int32_t rot, int32_t half,
+                         float magnitude, void *Y, int64_t ldy, int64_t ldyh, void *stream);
+
+/*
+ * sq_cache_append / sq_cache_read / sq_tree_attention -- keys and values in 4 bits.
+ *
+ * A row of K or V is Hk heads of D channels; every head is quantized for itself as a
+ * group of sq_quantize_grouped is (codes in [-8, 7], one fp16 step).  The cache is
+ * `pages` pages of `page` rows, one buffer per layer, owned by the caller;
+ * sq_cache_page_bytes is the size of a page (a multiple of 256; 0 for sizes that are
+ * not covered).  Layout of a page, nibbles holding code + 8, the even channel low:
+ *   - per head `page` D bytes: the codes of K, row after row (D / 2 bytes each), then
+ *     those of V in blocks of 16 rows, in a block [row / 4 % 4][unit][row % 4], a unit
+ *     being D / 16 neighbouring channels (unit u: channels u D / 16 ..);
+ *   - then the steps, fp16: K [Hk][page], V [Hk][page].
+ *
+ * Sequence b of B owns the new rows row_start[b] .. row_start[b + 1] - 1 of the
+ * call's T rows; they follow the cached[b] rows it has already, and its row number p
+ * is in slot p % page of page table[b, p / page].
+ *   Hk         heads of K and V, 1 .. SQ_CACHE_MAX_HEADS; D 64, 128 or 256
+ *   page       a power of two, 16 .. 1024; pages >= 0
+ *   B          0 .. SQ_CACHE_MAX_SEQUENCES
+ *   row_start  device, int32 [B + 1], not decreasing
+ *   cached     device, int32 [B]
+ *   table      device, int32 [B, per_sequence]; page * per_sequence < 2^31
+ *   cache      device, pages * sq_cache_page_bytes bytes, 16-byte aligned
+ * The device arrays are read by the kernels only, so a captured graph goes with
+ * their contents.  What they name is checked there: rows in front of row_start[0] or
+ * from row_start[B] on, rows beyond per_sequence pages, and page numbers outside
+ * [0, pages) are left out (not written, not read, not attended to).
+ *
+ * sq_cache_append   quantizes the new rows of K and V (device, fp16, head h of row t at
+ *              t * ldk + h * D, 16-byte aligned, ldk % 8 == 0; V likewise) into their
+ *              slots.  Two rows with the same slot (a page that two sequences of the
+ *              call write to) leave a mix of both there.
+ * sq_cache_read     the same rows back, K and V device out, fp16( code * step ); rows
+ *              that are left out keep what they held.
+ */
+#define SQ_CACHE_MAX_HEADS 256
+#define SQ_CACHE_MAX_SEQUENCES 65535
+int64_t sq_cache_page_bytes(int32_t Hk, int32_t D, int32_t page);
+sq_status sq_cache_append(const void *K, int64_t ldk, const void *V, int64_t ldv, int64_t T,
+                          int32_t Hk, int32_t D, const int32_t *row_start, const int32_t *cached,
+                          int32_t B, const int32_t *table, int32_t per_sequence, int32_t page,
+                          void *cache, int32_t pages, void *stream);
+sq_status sq_cache_read(const void *cache, int32_t pages, int32_t Hk, int32_t D,
+                        const int32_t *row_start, const int32_t *cached, int32_t B,
+                        const int32_t *table, int32_t per_sequence, int32_t page,
+                        void *K, int64_t ldk, void *V, int64_t ldv, int64_t T, void *stream);
+
+/*
+ * sq_tree_attention -- attention of the new rows over the cache, which holds their own
+ * keys and values already (sq_cache_append first):
+ *
+ *   O[t, h] = sum_j softmax_j( scale * Q[t, h] . k_j ) v_j       over the rows j it sees
+ *
+ * New row i of sequence b sees the cached[b] rows before all new ones and, of the new
+ * ones, those whose bit is set in mask[t] (bit j: new row j; a token of a drafted tree
+ * sets its ancestors' bits and its own), or without a mask the rows 0 .. i (one token,
+ * a chain, a prompt).  A row that sees nothing gives zeros.
+ *   Q, O       device, fp16, head h of row t at t * ldq + h * D; 16-byte aligned,
+ *              ldq % 8 == 0; O likewise (ldo), not overlapping Q
+ *   Hq         query heads, a multiple of Hk; head h reads head h / (Hq / Hk) of K, V
+ *   mask       device, uint64 [T], or NULL.  With a mask a sequence has at most 64 new
+ *              rows (further ones are not seen by any).
+ *   max_rows   at least the new rows of every sequence (those from max_rows on are left
+ *              out: their rows of O keep what they held); <= 64 with a mask
+ *   max_keys   about the longest cached[b] + new rows: how finely the work is split.
+ *              Any value gives the right result.
+ *   scale      > 0
+ *   workspace  device, 16-byte aligned, workspace_bytes long, or NULL and 0.  The sums
+ *              of a split sequence meet in it; with less than
+ *              sq_tree_attention_workspace_bytes the work is split less.  Nothing in
+ *              it outlives the call; calls that may overlap need one each.
+ * O is a function of the arguments alone: no atomics, sums in a fixed order for given
+ * sizes.  T == 0, B == 0 or max_rows == 0 is legal and enqueues nothing.
+ */
+int64_t sq_tree_attention_workspace_bytes(int64_t T, int32_t Hq, int32_t D);
+sq_status sq_tree_attention(const void *Q, int64_t ldq, int64_t T, int32_t Hq, int32_t Hk, int32_t D,
+                            const int32_t *row_start, const int32_t *cached, int32_t B,
+                            const uint64_t *mask, int32_t max_rows, int32_t max_keys,
+                            const int32_t *table, int32_t per_sequence, int32_t page,
+                            const void *cache, int32_t pages, float scale, void *O, int64_t ldo,
+                            void *workspace, int64_t workspace_bytes, void *stream);
+
+/*
  * sq_kron_factor -- Kronecker dimension factorization (Alg. 1): n2 is the power
  * of two dividing n that lies closest to sqrt(n) (of two equally close ones the
  * smaller), n1 = n / n2.  Host only; n >= 1.

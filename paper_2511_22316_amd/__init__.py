@@ -9,10 +9,17 @@ from . import synth  # noqa: F401
 from . import binding  # noqa: F401
 from .binding import (  # noqa: F401
     SQError,
+    SQ_ROTARY_BASE,
+    SQ_ROTARY_LINEAR,
+    SQ_ROTARY_PARTS,
+    SQ_ROTARY_PLAIN,
     library_path,
     sq_build_rotation,
     sq_debug_set_option,
     sq_build_rotation_workspace_bytes,
+    sq_cache_append,
+    sq_cache_page_bytes,
+    sq_cache_read,
     sq_decode_layer,
     sq_decode_layer_static,
     sq_decode_layer_status,
@@ -23,15 +30,21 @@ from .binding import (  # noqa: F401
     sq_prepare_weights,
     sq_prepare_weights_variant,
     sq_prepared_rotation_bytes,
+    sq_quantize_grouped,
+    sq_rotary_fp16,
+    sq_rotary_table,
     sq_rotate_fp16,
     sq_rotate_quantize,
     sq_rotate_quantize_prepared,
     sq_rotate_quantize_variant,
+    sq_tree_attention,
+    sq_tree_attention_workspace_bytes,
     sq_w3a16_gemm,
     sq_w4a4_gemm,
     sq_w4a4_gemm_decode,
     sq_tile_weights_decode,
     sq_decode_weights_bytes,
     sq_w4a16_gemm,
+    sq_w4a16_gemm_grouped,
     sq_status_string,
 )

@@ -128,6 +128,37 @@ def _load():
         lib.sq_debug_rotq_plan.argtypes = [C.c_void_p, C.c_void_p, C.c_int32, C.c_int32] + [C.c_void_p] * 8
         lib.sq_debug_set_option.restype = C.c_int
         lib.sq_debug_set_option.argtypes = [C.c_int, C.c_int32]
+        lib.sq_quantize_grouped.restype = C.c_int
+        lib.sq_quantize_grouped.argtypes = [
+            C.c_void_p, C.c_int64, C.c_int32, C.c_int64, C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p]
+        lib.sq_w4a16_gemm_grouped.restype = C.c_int
+        lib.sq_w4a16_gemm_grouped.argtypes = [
+            C.c_void_p, C.c_int64, C.c_int32, C.c_int64, C.c_void_p, C.c_void_p, C.c_int32, C.c_int32,
+            C.c_void_p, C.c_int64, C.c_void_p]
+        lib.sq_rotary_table.restype = C.c_int
+        lib.sq_rotary_table.argtypes = [
+            C.c_int32, C.c_double, C.c_int, C.c_double, C.c_double, C.c_double, C.c_double, C.c_void_p]
+        lib.sq_rotary_fp16.restype = C.c_int
+        lib.sq_rotary_fp16.argtypes = [
+            C.c_void_p, C.c_int64, C.c_int32, C.c_int32, C.c_int64, C.c_int64,
+            C.c_void_p, C.c_void_p, C.c_int32, C.c_int32, C.c_float, C.c_void_p, C.c_int64, C.c_int64, C.c_void_p]
+        lib.sq_cache_page_bytes.restype = C.c_int64
+        lib.sq_cache_page_bytes.argtypes = [C.c_int32, C.c_int32, C.c_int32]
+        lib.sq_cache_append.restype = C.c_int
+        lib.sq_cache_append.argtypes = [
+            C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_int64, C.c_int32, C.c_int32,
+            C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p, C.c_int32, C.c_int32, C.c_void_p, C.c_int32, C.c_void_p]
+        lib.sq_cache_read.restype = C.c_int
+        lib.sq_cache_read.argtypes = [
+            C.c_void_p, C.c_int32, C.c_int32, C.c_int32, C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p, C.c_int32,
+            C.c_int32, C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_int64, C.c_void_p]
+        lib.sq_tree_attention_workspace_bytes.restype = C.c_int64
+        lib.sq_tree_attention_workspace_bytes.argtypes = [C.c_int64, C.c_int32, C.c_int32]
+        lib.sq_tree_attention.restype = C.c_int
+        lib.sq_tree_attention.argtypes = [
+            C.c_void_p, C.c_int64, C.c_int64, C.c_int32, C.c_int32, C.c_int32,
+            C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p, C.c_int32, C.c_int32, C.c_void_p, C.c_int32, C.c_int32,
+            C.c_void_p, C.c_int32, C.c_float, C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_void_p]
         lib.sq_kron_factor.restype = C.c_int
         lib.sq_kron_factor.argtypes = [C.c_int32, C.POINTER(C.c_int32), C.POINTER(C.c_int32)]
         lib.sq_build_rotation.restype = C.c_int
@@ -423,6 +454,169 @@ def sq_prepare_weights_variant(W, giv_i, giv_j, giv_theta, R1, R2, bits, clip_ra
         _dev_ptr(R1), int(R1.shape[0]), _dev_ptr(R2), int(R2.shape[0]), int(bits), float(clip_ratio),
         _dev_ptr(workspace), _dev_ptr(Qw), _dev_ptr(sw), _stream_handle(stream))
     _check(code)
+
+
+def _is(t, dtype, name, contiguous=True):
+    """Integer arrays and steps travel as bare pointers: their type and layout are checked here."""
+    if t.dtype is not dtype:
+        raise ValueError(f"{name} must be {dtype}")
+    if contiguous and not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+
+
+def _heads(t, name, dtype):
+    """[T, H, D] whose heads have contiguous channels: T, H, D, token stride, head stride."""
+    T, H, D = t.shape
+    if t.dtype is not dtype:
+        raise ValueError(f"{name} must be {dtype}")
+    if D > 1 and t.stride(2) != 1:
+        raise ValueError(f"{name}: the channels of a head must be contiguous")
+    head = t.stride(1) if H > 1 else D
+    return T, H, D, (t.stride(0) if T > 1 else max(H - 1, 0) * head + D), head
+
+
+def _packed_heads(t, name):
+    """_heads of fp16 rows whose heads lie side by side; a row's stride is a multiple of 8 in any case."""
+    T, H, D, ld, head = _heads(t, name, _torch.float16)
+    if head != D:
+        raise ValueError(f"{name}: the heads of a row must lie side by side")
+    return T, H, D, ld
+
+
+def sq_quantize_grouped(X, group, Q, steps, stream=None) -> None:
+    """X fp16 [T, K] to codes Q uint8 [T, K/2] with steps fp16 [T, K / group]."""
+    lib = _load()
+    T, K = X.shape
+    _is(X, _torch.float16, "X", False)
+    _is(Q, _torch.uint8, "Q")
+    _is(steps, _torch.float16, "steps")
+    if group <= 0 or tuple(Q.shape) != (T, K // 2) or tuple(steps.shape) != (T, K // group):
+        raise ValueError("Q must be [T, K/2] and steps [T, K / group]")
+    if K > 1 and X.stride(1) != 1:
+        raise ValueError("the channels of X must be contiguous")
+    _check(lib.sq_quantize_grouped(X.data_ptr(), T, K, X.stride(0) if T > 1 else K, int(group), Q.data_ptr(),
+                                   steps.data_ptr(), _stream_handle(stream)))
+
+
+def sq_w4a16_gemm_grouped(X, Qw, steps, Y, stream=None) -> None:
+    """X fp16 [T, K] times weight codes Qw uint8 [N, K/2] with steps fp16 [N, K / group] -> Y fp16 [T, N]; the group is
+    what the shapes say."""
+    lib = _load()
+    T, K = X.shape
+    N, groups = steps.shape
+    _is(X, _torch.float16, "X", False)
+    _is(Y, _torch.float16, "Y", False)
+    _is(Qw, _torch.uint8, "Qw")
+    _is(steps, _torch.float16, "steps")
+    if groups <= 0 or K % groups or tuple(Qw.shape) != (N, K // 2) or tuple(Y.shape) != (T, N):
+        raise ValueError("Qw must be [N, K/2], steps [N, K / group] and Y [T, N]")
+    if (K > 1 and X.stride(1) != 1) or (N > 1 and Y.stride(1) != 1):
+        raise ValueError("the rows of X and Y must be contiguous")
+    _check(lib.sq_w4a16_gemm_grouped(X.data_ptr(), T, K, X.stride(0) if T > 1 else K, Qw.data_ptr(), steps.data_ptr(),
+                                     K // groups, N, Y.data_ptr(), Y.stride(0) if T > 1 else max(N, 1), _stream_handle(stream)))
+
+
+# sq_rotary_scaling of singlequant.h
+SQ_ROTARY_PLAIN = 0
+SQ_ROTARY_LINEAR = 1
+SQ_ROTARY_BASE = 2
+SQ_ROTARY_PARTS = 3
+
+
+def sq_rotary_table(rot, base=10000.0, scaling=SQ_ROTARY_PLAIN, factor=1.0, trained=0.0, low=0.0, high=0.0):
+    """The frequencies of rot / 2 pairs as fractions of a turn in units of 2^-64: int64 [rot / 2] on the host (the bits of
+    the unsigned numbers), to be copied to the device for sq_rotary_fp16."""
+    lib = _load()
+    rot = int(rot)
+    turns = np.zeros(max(rot, 0) // 2, np.int64)
+    _check(lib.sq_rotary_table(rot, float(base), int(scaling), float(factor), float(trained), float(low), float(high),
+                               turns.ctypes.data))
+    return _torch.from_numpy(turns)
+
+
+def sq_rotary_fp16(X, positions, turns, half, Y, magnitude=1.0, stream=None) -> None:
+    """Rotary positions on X fp16 [T, H, D] (any token and head strides) -> Y of the same shape (may be X).  positions
+    int32 [T]; turns int64 [rot / 2] on the device, from sq_rotary_table; half: pairs (i, i + rot / 2), else (2i, 2i + 1)."""
+    lib = _load()
+    T, H, D, ldx, ldh = _heads(X, "X", _torch.float16)
+    _, _, _, ldy, ldyh = _heads(Y, "Y", _torch.float16)
+    _is(positions, _torch.int32, "positions")
+    _is(turns, _torch.int64, "turns")
+    if Y.shape != X.shape or positions.numel() != T:
+        raise ValueError("Y must have the shape of X, positions one entry per token")
+    _check(lib.sq_rotary_fp16(X.data_ptr(), T, H, D, ldx, ldh, positions.data_ptr(), turns.data_ptr(), 2 * turns.numel(),
+                              1 if half else 0, float(magnitude), Y.data_ptr(), ldy, ldyh, _stream_handle(stream)))
+
+
+@functools.lru_cache(maxsize=256)
+def sq_cache_page_bytes(Hk: int, D: int, page: int) -> int:
+    return int(_load().sq_cache_page_bytes(int(Hk), int(D), int(page)))
+
+
+def _cache_args(T, Hk, D, row_start, cached, table, page, cache):
+    """B, per_sequence and pages of a cache (any uint8 tensor that is a whole number of pages)."""
+    _is(row_start, _torch.int32, "row_start")
+    _is(cached, _torch.int32, "cached")
+    _is(table, _torch.int32, "table")
+    _is(cache, _torch.uint8, "cache")
+    B, per_sequence = table.shape
+    if row_start.numel() != B + 1 or cached.numel() != B:
+        raise ValueError("table must be [B, pages of a sequence], row_start [B + 1] and cached [B]")
+    size = sq_cache_page_bytes(Hk, D, page)
+    if size and cache.numel() % size:
+        raise ValueError("cache is not a whole number of pages of sq_cache_page_bytes")
+    return B, per_sequence, cache.numel() // size if size else 0
+
+
+def sq_cache_append(K, V, row_start, cached, table, page, cache, stream=None) -> None:
+    """New rows K, V fp16 [T, Hk, D] (any row strides) into the cache: row_start int32 [B + 1], cached int32 [B], table
+    int32 [B, pages of a sequence], cache uint8, pages * sq_cache_page_bytes(Hk, D, page) bytes."""
+    lib = _load()
+    T, Hk, D, ldk = _packed_heads(K, "K")
+    _, _, _, ldv = _packed_heads(V, "V")
+    if V.shape != K.shape:
+        raise ValueError("K and V must have the same shape")
+    B, per_sequence, pages = _cache_args(T, Hk, D, row_start, cached, table, page, cache)
+    _check(lib.sq_cache_append(K.data_ptr(), ldk, V.data_ptr(), ldv, T, Hk, D, row_start.data_ptr(), cached.data_ptr(), B,
+                               table.data_ptr(), per_sequence, int(page), cache.data_ptr(), pages, _stream_handle(stream)))
+
+
+def sq_cache_read(cache, row_start, cached, table, page, K, V, stream=None) -> None:
+    """The rows that sq_cache_append with the same arrays writes, as fp16 into K, V [T, Hk, D]."""
+    lib = _load()
+    T, Hk, D, ldk = _packed_heads(K, "K")
+    _, _, _, ldv = _packed_heads(V, "V")
+    if V.shape != K.shape:
+        raise ValueError("K and V must have the same shape")
+    B, per_sequence, pages = _cache_args(T, Hk, D, row_start, cached, table, page, cache)
+    _check(lib.sq_cache_read(cache.data_ptr(), pages, Hk, D, row_start.data_ptr(), cached.data_ptr(), B, table.data_ptr(),
+                             per_sequence, int(page), K.data_ptr(), ldk, V.data_ptr(), ldv, T, _stream_handle(stream)))
+
+
+def sq_tree_attention_workspace_bytes(T: int, Hq: int, D: int) -> int:
+    return int(_load().sq_tree_attention_workspace_bytes(int(T), int(Hq), int(D)))
+
+
+def sq_tree_attention(Q, row_start, cached, mask, table, page, cache, Hk, scale, O, workspace=None, max_rows=1, max_keys=None,
+                      stream=None) -> None:
+    """Attention of the new rows Q fp16 [T, Hq, D] over the cache -> O [T, Hq, D].  mask int64 [T] (bit j: the row sees new
+    row j of its sequence) or None (rows 0 .. i); max_rows: at least the new rows of every sequence; max_keys: about the
+    longest sequence (None: what the table holds); workspace: any device tensor, or None (nothing is split)."""
+    lib = _load()
+    T, Hq, D, ldq = _packed_heads(Q, "Q")
+    _, _, _, ldo = _packed_heads(O, "O")
+    if O.shape != Q.shape:
+        raise ValueError("O must have the shape of Q")
+    B, per_sequence, pages = _cache_args(T, Hk, D, row_start, cached, table, page, cache)
+    if mask is not None:
+        _is(mask, _torch.int64, "mask")
+        if mask.numel() != T:
+            raise ValueError("mask must have one word per row")
+    _check(lib.sq_tree_attention(
+        Q.data_ptr(), ldq, T, Hq, Hk, D, row_start.data_ptr(), cached.data_ptr(), B,
+        None if mask is None else mask.data_ptr(), int(max_rows), per_sequence * page if max_keys is None else int(max_keys),
+        table.data_ptr(), per_sequence, int(page), cache.data_ptr(), pages, float(scale), O.data_ptr(), ldo,
+        _dev_ptr(workspace), 0 if workspace is None else workspace.numel() * workspace.element_size(), _stream_handle(stream)))
 
 
 def sq_kron_factor(n: int):

@@ -1,0 +1,185 @@
+// sq_rotary_fp16: rotary positions, a plane rotation of every pair of channels of a head by an angle that grows with the
+// token's position; sq_rotary_table: the frequencies, scaled for long contexts (host).
+#include "sq_common.h"
+
+#include <cmath>
+
+namespace sq {
+
+namespace {
+
+// Cosine and sine of position * frequency.  The frequency is a 64-bit fraction of a turn, so the product modulo 2^64 is
+// the fraction of a turn that is left of the angle, without error for any 32-bit position; its upper half goes to fp32
+// (2^-25 of a turn at most).
+__device__ __forceinline__ void rotation_of(int position, uint64_t turns, float magnitude, float &c, float &s)
+{
+    const uint64_t angle = (uint64_t)(int64_t)position * turns;
+    const float half_turns = (float)(int32_t)(angle >> 32) * 0x1p-31f;
+    sincospif(half_turns, &s, &c);
+    c *= magnitude;
+    s *= magnitude;
+}
+
+__device__ __forceinline__ uint32_t pack_halves(float a, float b)
+{
+    const v2h p = {(_Float16)a, (_Float16)b};
+    return __builtin_bit_cast(uint32_t, p);
+}
+
+// A lane owns eight pairs of a token's heads: channels 8 u .. and rot / 2 + 8 u .. (HALF), or 16 u .. 16 u + 15.  It takes
+// their cosines and sines once and then walks over the heads slot, slot + slots, ...  Behind the rot / 16 units of pairs
+// come units of 16 channels that are copied (tail; none where Y is X).  One read and one write of the rows: HBM-bound; the
+// angles are shared by the heads of a slot, and the slots are as many as fill the chip.
+template <bool HALF>
+__global__ __launch_bounds__(256) void rotary_kernel(const __half *X, int64_t T, int H, int D, int64_t ldx, int64_t ldh,
+                                                     const int32_t *__restrict__ positions, const uint64_t *__restrict__ turns,
+                                                     int rot, float magnitude, __half *Y, int64_t ldy, int64_t ldyh, int units,
+                                                     int slots)
+{
+    const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    const int per_token = units * slots;
+    const int64_t t = id / per_token;
+    if (t >= T) return;
+    const int rest = (int)(id - t * per_token), u = rest % units, slot = rest / units;
+    const __half *x = X + t * ldx;
+    __half *y = Y + t * ldy;
+    if (u >= rot / 16) {
+        const int d = rot + 16 * (u - rot / 16);
+        for (int h = slot; h < H; h += slots)
+#pragma unroll
+            for (int k = 0; k < 2; ++k)
+                if (d + 8 * k < D)
+                    *reinterpret_cast<uint4 *>(y + h * ldyh + d + 8 * k) = *reinterpret_cast<const uint4 *>(x + h * ldh + d + 8 * k);
+        return;
+    }
+    float c[8], s[8];
+    const int position = positions[t];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) rotation_of(position, turns[8 * u + e], magnitude, c[e], s[e]);
+    const int d0 = HALF ? 8 * u : 16 * u, d1 = HALF ? rot / 2 + 8 * u : 16 * u + 8;
+#pragma unroll 4
+    for (int h = slot; h < H; h += slots) {
+        const v8h a = *reinterpret_cast<const v8h *>(x + h * ldh + d0), b = *reinterpret_cast<const v8h *>(x + h * ldh + d1);
+        uint4 ya, yb;
+        uint32_t *wa = &ya.x, *wb = &yb.x;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            if constexpr (HALF) {
+                const int e = 2 * k, f = 2 * k + 1;
+                wa[k] = pack_halves((float)a[e] * c[e] - (float)b[e] * s[e], (float)a[f] * c[f] - (float)b[f] * s[f]);
+                wb[k] = pack_halves((float)b[e] * c[e] + (float)a[e] * s[e], (float)b[f] * c[f] + (float)a[f] * s[f]);
+            } else {
+                const int e = k, f = 4 + k;
+                wa[k] = pack_halves((float)a[2 * k] * c[e] - (float)a[2 * k + 1] * s[e],
+                                    (float)a[2 * k + 1] * c[e] + (float)a[2 * k] * s[e]);
+                wb[k] = pack_halves((float)b[2 * k] * c[f] - (float)b[2 * k + 1] * s[f],
+                                    (float)b[2 * k + 1] * c[f] + (float)b[2 * k] * s[f]);
+            }
+        }
+        *reinterpret_cast<uint4 *>(y + h * ldyh + d0) = ya;
+        *reinterpret_cast<uint4 *>(y + h * ldyh + d1) = yb;
+    }
+}
+
+// Any width and alignment: a lane takes one pair, or one copied channel, of one head.
+__global__ __launch_bounds__(256) void rotary_pair_kernel(const __half *X, int64_t T, int H, int D, int64_t ldx, int64_t ldh,
+                                                          const int32_t *__restrict__ positions,
+                                                          const uint64_t *__restrict__ turns, int rot, int half,
+                                                          float magnitude, __half *Y, int64_t ldy, int64_t ldyh, int units)
+{
+    const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    const int64_t row = id / units, t = row / H;
+    if (t >= T) return;
+    const int u = (int)(id - row * units), h = (int)(row - t * H);
+    const __half *x = X + t * ldx + h * ldh;
+    __half *y = Y + t * ldy + h * ldyh;
+    if (u >= rot / 2) {
+        y[rot / 2 + u] = x[rot / 2 + u];
+        return;
+    }
+    float c, s;
+    rotation_of(positions[t], turns[u], magnitude, c, s);
+    const int p = half ? u : 2 * u, q = half ? rot / 2 + u : 2 * u + 1;
+    const float a = __half2float(x[p]), b = __half2float(x[q]);
+    y[p] = __float2half_rn(a * c - b * s);
+    y[q] = __float2half_rn(b * c + a * s);
+}
+
+}  // namespace
+
+}  // namespace sq
+
+extern "C" sq_status sq_rotary_table(int32_t rot, double base, sq_rotary_scaling scaling, double factor, double trained,
+                                     double low, double high, uint64_t *turns)
+{
+    if (rot <= 0 || (rot % 2) != 0 || rot > SQ_ROTARY_MAX_CHANNELS || !(base > 1.0) || !(base <= 1e18)) return SQ_ERR_SHAPE;
+    const bool scaled = scaling != SQ_ROTARY_PLAIN;
+    if (scaling != SQ_ROTARY_PLAIN && scaling != SQ_ROTARY_LINEAR && scaling != SQ_ROTARY_BASE && scaling != SQ_ROTARY_PARTS)
+        return SQ_ERR_SHAPE;
+    if (scaled && (!(factor >= 1.0) || !(factor <= 1e9))) return SQ_ERR_SHAPE;
+    if (scaling == SQ_ROTARY_BASE && rot == 2) return SQ_ERR_SHAPE;       // its exponent divides by rot - 2
+    if (scaling == SQ_ROTARY_PARTS && (!(trained > 0.0) || !(low >= 0.0) || !(high > low) || !(high <= 1e18) || !(trained <= 1e18)))
+        return SQ_ERR_SHAPE;
+    if (!turns) return SQ_ERR_NULL;
+    const double two_pi = 6.283185307179586476925286766559;
+    if (scaling == SQ_ROTARY_BASE) base *= std::pow(factor, (double)rot / (double)(rot - 2));
+    for (int i = 0; i < rot / 2; ++i) {
+        double f = std::pow(base, -2.0 * i / rot);
+        if (scaling == SQ_ROTARY_LINEAR) f /= factor;
+        if (scaling == SQ_ROTARY_PARTS) {
+            double keep = (trained * f / two_pi - low) / (high - low);
+            keep = keep < 0.0 ? 0.0 : keep > 1.0 ? 1.0 : keep;
+            f = f * keep + f / factor * (1.0 - keep);
+        }
+        // f <= 1 radian: below 2^62 in units of 2^-64 of a turn
+        turns[i] = (uint64_t)std::nearbyint(f / two_pi * 18446744073709551616.0);
+    }
+    return SQ_OK;
+}
+
+extern "C" sq_status sq_rotary_fp16(const void *X, int64_t T, int32_t H, int32_t D, int64_t ldx, int64_t ldh,
+                                    const int32_t *positions, const uint64_t *turns, int32_t rot, int32_t half,
+                                    float magnitude, void *Y, int64_t ldy, int64_t ldyh, void *stream)
+{
+    if (T < 0 || T > SQ_MAX_ROWS || H < 0 || H > 65536 || D <= 0 || D > 65536 || rot < 0 || (rot % 2) != 0 || rot > D ||
+        rot > SQ_ROTARY_MAX_CHANNELS)
+        return SQ_ERR_SHAPE;
+    if (half != 0 && half != 1) return SQ_ERR_SHAPE;
+    const int64_t rows = (int64_t)(H > 0 ? H - 1 : 0);
+    if (ldh < D || ldyh < D || ldx < rows * ldh + D || ldy < rows * ldyh + D) return SQ_ERR_SHAPE;
+    if (T == 0 || H == 0) return SQ_OK;
+    if (!X || !Y || (rot > 0 && (!positions || !turns))) return SQ_ERR_NULL;
+    if (((uintptr_t)X & 1) || ((uintptr_t)Y & 1) || ((uintptr_t)positions & 3) || ((uintptr_t)turns & 7)) return SQ_ERR_ALIGN;
+    const bool in_place = X == Y;
+    if (in_place && (ldx != ldy || ldh != ldyh)) return SQ_ERR_SHAPE;
+    const __half *x = static_cast<const __half *>(X);
+    __half *y = static_cast<__half *>(Y);
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    const int copied = in_place ? 0 : D - rot;
+    if (rot == 0 && copied == 0) return SQ_OK;
+    const bool wide = (rot % 16) == 0 && (D % 8) == 0 && (ldx % 8) == 0 && (ldh % 8) == 0 && (ldy % 8) == 0 && (ldyh % 8) == 0 &&
+                      ((uintptr_t)X & 15) == 0 && ((uintptr_t)Y & 15) == 0;
+    if (wide) {
+        const int units = rot / 16 + (copied + 15) / 16;
+        // enough lanes that every SIMD of the chip holds four waves, and at least eight heads side by side in a row
+        const int64_t lanes = T * (int64_t)units;
+        int64_t want = (262144 + lanes - 1) / lanes;
+        if (want < 8) want = 8;
+        const int slots = (int)(want < H ? want : H);
+        const int64_t blocks = (lanes * slots + 255) / 256;
+        if (blocks > 0x7FFFFFFF) return SQ_ERR_SHAPE;
+        if (half)
+            hipLaunchKernelGGL(sq::rotary_kernel<true>, dim3((unsigned)blocks), dim3(256), 0, st, x, T, H, D, ldx, ldh, positions,
+                               turns, rot, magnitude, y, ldy, ldyh, units, slots);
+        else
+            hipLaunchKernelGGL(sq::rotary_kernel<false>, dim3((unsigned)blocks), dim3(256), 0, st, x, T, H, D, ldx, ldh, positions,
+                               turns, rot, magnitude, y, ldy, ldyh, units, slots);
+    } else {
+        const int units = rot / 2 + copied;
+        const int64_t blocks = (T * H * units + 255) / 256;
+        if (blocks > 0x7FFFFFFF) return SQ_ERR_SHAPE;
+        hipLaunchKernelGGL(sq::rotary_pair_kernel, dim3((unsigned)blocks), dim3(256), 0, st, x, T, H, D, ldx, ldh, positions, turns,
+                           rot, half, magnitude, y, ldy, ldyh, units);
+    }
+    return hipGetLastError() == hipSuccess ? SQ_OK : SQ_ERR_LAUNCH;
+}
