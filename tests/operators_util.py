@@ -99,7 +99,8 @@ def attention(q, k, v, sk, sv, sees, scale):
     Scores: products of fp16 and nibbles plus 8 (16 |q| bounds a term), D / 32 steps of 32, the offset taken off, then four
     fp32 roundings; delta is the largest error of a score in natural units, so that a weight is off by a factor within
     exp(+-2 delta) (its own and the normaliser's) beside 6 roundings.  A weight times the value's step is rounded to fp16:
-    half a step of fp16, or 2^-25 below its normal range where the largest weight times the largest step is at least 2^-2.
+    half a step of fp16, or 2^-25 below its normal range.  The largest such product P is at least 2^-1, and with l the
+    normaliser on the same scale sum(p sv) >= P / l, so n keys of codes up to 8 are off by n 8 2^-25 / l <= n 2^-21 sum(p sv).
     The sums of weights and nibbles plus 8 (16 steps bound a term) take L / 32 steps of 32 per part and as many to add the
     parts.  One rounding to fp16 at the end."""
     n, D = q.shape
@@ -121,9 +122,8 @@ def attention(q, k, v, sk, sv, sees, scale):
     delta = scale * (D // 32 + 33) * EPS32 * 16 * np.abs(qq).sum(1, keepdims=True) * np.where(see, sk, 0).max(1, keepdims=True) \
         + 6 * EPS32 * np.abs(np.where(see, s, 0)).max(1, keepdims=True)
     mags = p @ np.abs(v)
-    biggest = np.where(see, sv, 0).max(1, keepdims=True)
     slack = (2 * delta + HALF + 8 * EPS32) * mags + (L // 32 + 40) * EPS32 * 16 * (p @ sv)[:, None] \
-        + see.sum(1, keepdims=True) / l * 2.0 ** -25 * 8 * 4 * biggest
+        + see.sum(1, keepdims=True) * 2.0 ** -21 * (p @ sv)[:, None]
     bound[some] = slack + HALF * (np.abs(O[some]) + slack) + TINY
     return O, bound
 
