@@ -41,38 +41,30 @@ __device__ __forceinline__ void sort_steps(uint32_t (&w)[4])
     }
 }
 
-// The steps of a slice's groups for one channel: one fp16, or the pair or four that lie side by side (2-byte aligned).
-template <int GROUP>
-struct SliceSteps {
-    static constexpr int COUNT = GROUP >= 128 ? 1 : 128 / GROUP;
-    struct __attribute__((packed, aligned(2))) Raw {
-        _Float16 s[COUNT];
-    } raw;
-    __device__ __forceinline__ void load(const __half *row, int slice, int group)
-    {
-        raw = *reinterpret_cast<const Raw *>(row + (GROUP >= 128 ? 128 * slice / group : COUNT * slice));
-    }
-};
-
-// 16 NS channels per workgroup and TT blocks of 16 tokens; the NW waves deal the slices of K among themselves and add up
-// through LDS.  Everything goes global -> registers, D slices ahead.
-template <int GROUP, int NS, int NW, int TT, int D>
+// 16 NS channels and TT blocks of 16 tokens per workgroup; the NW waves deal the slices of K among themselves and add up
+// through LDS.  Everything goes global -> registers, one unit of H slices ahead.  The steps of a unit are one load: every
+// load of a wave touches 16 rows, and their number is what this kernel costs beside the bytes.
+template <int GROUP, int NS, int NW, int TT, int H>
 __global__ __launch_bounds__(NW *kWave) void w4a16_grouped_skinny_kernel(const __half *__restrict__ X, int64_t ldx, int T, int K,
                                                                          const uint8_t *__restrict__ Qw,
-                                                                         const __half *__restrict__ steps, int group, int N,
+                                                                         const __half *__restrict__ steps, int N,
                                                                          __half *__restrict__ Y, int64_t ldy)
 {
-    constexpr int SUB = SliceSteps<GROUP>::COUNT, CHAIN = 4 / SUB;       // groups of a slice, steps of one
+    constexpr int SUB = GROUP >= 128 ? 1 : 128 / GROUP, CHAIN = 4 / SUB;       // groups of a slice, steps of one
+    constexpr int SPU = H * 128 < GROUP ? 1 : H * 128 / GROUP;                 // groups of a unit
+    struct __attribute__((packed, aligned(2))) UnitSteps {
+        _Float16 s[SPU];
+    };
     __shared__ float red[NW][NS][TT][4][kWave];
     const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid / kWave;
     const int l16 = lane & 15, q = lane >> 4;
-    const int col0 = blockIdx.x * (16 * NS), groups = K / group, slices = (K + 127) / 128;
+    const int col0 = blockIdx.x * (16 * NS), t0 = blockIdx.y * (16 * TT), groups = K / GROUP, units = (K + 128 * H - 1) / (128 * H);
 
     // rows past the ends are clamped: their products are never stored
     const __half *x_row[TT], *s_row[NS];
     const uint8_t *w_row[NS];
 #pragma unroll
-    for (int i = 0; i < TT; ++i) x_row[i] = X + (int64_t)min(16 * i + l16, T - 1) * ldx;
+    for (int i = 0; i < TT; ++i) x_row[i] = X + (int64_t)min(t0 + 16 * i + l16, T - 1) * ldx;
 #pragma unroll
     for (int c = 0; c < NS; ++c) {
         const int64_t n = min(col0 + 16 * c + l16, N - 1);
@@ -85,84 +77,93 @@ __global__ __launch_bounds__(NW *kWave) void w4a16_grouped_skinny_kernel(const _
 #pragma unroll
         for (int i = 0; i < TT; ++i) total[c][i] = v4f{0.f, 0.f, 0.f, 0.f};
 
-    uint4 w[D][NS];
-    SliceSteps<GROUP> s[D][NS];
-    v8h x[D][TT][4];
-    auto fetch = [&](int set, int slice) {
+    auto step_at = [&](int unit) { return unit * (128 * H) / GROUP; };
+    uint4 w[2][NS][H];
+    UnitSteps s[2][NS];
+    v8h x[2][TT][H][4];
+    auto fetch = [&](int set, int unit) {
 #pragma unroll
         for (int c = 0; c < NS; ++c) {
-            w[set][c] = *reinterpret_cast<const uint4 *>(w_row[c] + slice * 64 + 16 * q);
-            s[set][c].load(s_row[c], slice, group);
+#pragma unroll
+            for (int h = 0; h < H; ++h) w[set][c][h] = *reinterpret_cast<const uint4 *>(w_row[c] + unit * (64 * H) + 64 * h + 16 * q);
+            s[set][c] = *reinterpret_cast<const UnitSteps *>(s_row[c] + step_at(unit));
         }
 #pragma unroll
         for (int i = 0; i < TT; ++i)
 #pragma unroll
-            for (int j = 0; j < 4; ++j) x[set][i][j] = *reinterpret_cast<const v8h *>(x_row[i] + slice * 128 + slice_place<GROUP>(j, q));
+            for (int h = 0; h < H; ++h)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) x[set][i][h][j] = *reinterpret_cast<const v8h *>(x_row[i] + unit * (128 * H) + 128 * h + slice_place<GROUP>(j, q));
+    };
+    // the unit that ends behind the row: codes from inside it, tokens and steps of zero
+    auto fetch_last = [&](int unit) {
+#pragma unroll
+        for (int c = 0; c < NS; ++c) {
+#pragma unroll
+            for (int h = 0; h < H; ++h) w[0][c][h] = *reinterpret_cast<const uint4 *>(w_row[c] + min(unit * (64 * H) + 64 * h + 16 * q, K / 2 - 16));
+#pragma unroll
+            for (int g = 0; g < SPU; ++g)
+                s[0][c].s[g] = step_at(unit) + g < groups ? (_Float16)__half2float(s_row[c][step_at(unit) + g]) : (_Float16)0.f;
+        }
+#pragma unroll
+        for (int i = 0; i < TT; ++i)
+#pragma unroll
+            for (int h = 0; h < H; ++h)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const int at = unit * (128 * H) + 128 * h + slice_place<GROUP>(j, q);
+                    x[0][i][h][j] = v8h{0, 0, 0, 0, 0, 0, 0, 0};
+                    if (at < K) x[0][i][h][j] = *reinterpret_cast<const v8h *>(x_row[i] + at);
+                }
     };
     uint32_t magic;                                    // 1024.0 in both halves, held in a vector register
     asm volatile("v_mov_b32 %0, 0x64006400" : "=v"(magic));
     auto multiply = [&](int set) {
 #pragma unroll
-        for (int c = 0; c < NS; ++c) {
-            uint32_t d[4] = {w[set][c].x, w[set][c].y, w[set][c].z, w[set][c].w};
-            sort_steps<GROUP>(d);
+        for (int h = 0; h < H; ++h) {
+            v8h a[TT][4];
 #pragma unroll
-            for (int g = 0; g < SUB; ++g) {
-                v4f part[TT];
+            for (int i = 0; i < TT; ++i)
 #pragma unroll
-                for (int j = g * CHAIN; j < (g + 1) * CHAIN; ++j) {
-                    const v8h b = widen_codes_f16(d[j], magic);
+                for (int j = 0; j < 4; ++j) a[i][j] = __builtin_bit_cast(v8h, interleave_halves(__builtin_bit_cast(uint4, x[set][i][h][j])));
 #pragma unroll
-                    for (int i = 0; i < TT; ++i) {
-                        const v8h a = __builtin_bit_cast(v8h, interleave_halves(__builtin_bit_cast(uint4, x[set][i][j])));
-                        part[i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, j == g * CHAIN ? v4f{0.f, 0.f, 0.f, 0.f} : part[i], 0, 0, 0);
+            for (int c = 0; c < NS; ++c) {
+                uint32_t d[4] = {w[set][c][h].x, w[set][c][h].y, w[set][c][h].z, w[set][c][h].w};
+                sort_steps<GROUP>(d);
+#pragma unroll
+                for (int g = 0; g < SUB; ++g) {
+                    v4f part[TT];
+#pragma unroll
+                    for (int j = g * CHAIN; j < (g + 1) * CHAIN; ++j) {
+                        const v8h b = widen_codes_f16(d[j], magic);
+#pragma unroll
+                        for (int i = 0; i < TT; ++i)
+                            part[i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(a[i][j], b, j == g * CHAIN ? v4f{0.f, 0.f, 0.f, 0.f} : part[i], 0, 0, 0);
                     }
+                    const float step = (float)s[set][c].s[h * SPU / H + g];
+#pragma unroll
+                    for (int i = 0; i < TT; ++i)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) total[c][i][e] = __builtin_fmaf(step, part[i][e], total[c][i][e]);
                 }
-                const float step = (float)s[set][c].raw.s[g];
-#pragma unroll
-                for (int i = 0; i < TT; ++i)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) total[c][i][e] = __builtin_fmaf(step, part[i][e], total[c][i][e]);
             }
         }
     };
-    // wave w takes slices w, w + NW, ..; behind its last one that one is requested again, and dropped
-    const int whole = K / 128;
-    int S = wave;
-    if (S < whole) {
-        const int last = S + (whole - 1 - S) / NW * NW;
-#pragma unroll
-        for (int k = 0; k < D - 1; ++k) fetch(k, min(S + k * NW, last));
-        while (true) {
-            bool more = true;
-#pragma unroll
-            for (int k = 0; k < D; ++k) {
-                fetch((k + D - 1) % D, min(S + (D - 1) * NW, last));
-                multiply(k);
-                S += NW;
-                if (S > last) {
-                    more = false;
-                    break;
-                }
-            }
-            if (!more) break;
-        }
+    // wave w takes units w, w + NW, ..; two register sets alternate
+    const int whole = K / (128 * H);
+    int P = wave;
+    if (P < whole) fetch(0, P);
+    while (P < whole) {
+        if (P + NW < whole) fetch(1, P + NW);
+        multiply(0);
+        P += NW;
+        if (P >= whole) break;
+        if (P + NW < whole) fetch(0, P + NW);
+        multiply(1);
+        P += NW;
     }
-    // half a slice at the end of a row (groups of 32 or 64): its second half is read as the first and multiplied by 0
-    if (GROUP < 128 && whole < slices && wave == whole % NW) {
-#pragma unroll
-        for (int c = 0; c < NS; ++c) {
-            w[0][c] = *reinterpret_cast<const uint4 *>(w_row[c] + whole * 64 + 16 * (q & 1));
-#pragma unroll
-            for (int g = 0; g < SUB; ++g) s[0][c].raw.s[g] = g < SUB / 2 ? __half2float(s_row[c][SUB * whole + g]) : 0.f;
-        }
-#pragma unroll
-        for (int i = 0; i < TT; ++i)
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                x[0][i][j] = *reinterpret_cast<const v8h *>(x_row[i] + whole * 128 + slice_place<GROUP>(j, q) % 64);
-                if (j >= 2) x[0][i][j] = v8h{0, 0, 0, 0, 0, 0, 0, 0};
-            }
+    if (whole < units && wave == whole % NW) {
+        fetch_last(whole);
         multiply(0);
     }
 
@@ -179,9 +180,198 @@ __global__ __launch_bounds__(NW *kWave) void w4a16_grouped_skinny_kernel(const _
         float sum = 0.f;
 #pragma unroll
         for (int v = 0; v < NW; ++v) sum += red[v][c][i][e][ln];
-        const int t = 16 * i + 4 * (ln >> 4) + e, n = col0 + 16 * c + (ln & 15);
+        const int t = t0 + 16 * i + 4 * (ln >> 4) + e, n = col0 + 16 * c + (ln & 15);
         if (t < T && n < N) Y[(int64_t)t * ldy + n] = __float2half_rn(sum);
     }
+}
+
+// ---- at most 16 tokens whose rows fit in LDS ------------------------------------------------------
+// In the kernel above every workgroup fetches the token rows for itself, twice to sixteen times the bytes of the codes it
+// reads.  Here a workgroup copies the rows into LDS once (each 16-byte chunk already in the order the widened codes
+// take).  It owns blocks of 16 channels (b % grid), whose rounds of NR slices its NW waves share evenly, one run of rounds
+// each; what a run leaves of a block is added up at the end, in the order of the waves.  A slice of the next round is
+// requested when this round's is done, so a wave has NR KB of codes in flight at all times, across the ends of blocks too.
+// The steps of a round are one load: every quarter of a wave takes a quarter of them, and swaps hand them to the others.
+// (A step load per slice touches 16 cache lines for two bytes of each, which the codes have pushed out of the CU's cache
+// again by the next slice: 43 us at T = 8, K = 8192, N = 28672, groups of 128; all steps of a round in every quarter
+// 33.5, and 46 with groups of 32.)  Where K is no whole number of rounds the last slice is taken again with steps of zero.
+constexpr int kRowPad = 16;            // bytes; sixteen rows then start in sixteen different 16-byte bank groups
+
+// A dword of every quarter of the wave, in all of them.
+__device__ __forceinline__ void all_quarters(uint32_t v, uint32_t (&of)[4])
+{
+    typedef uint32_t v2u __attribute__((ext_vector_type(2)));
+    const v2u halves = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+    const uint32_t lower = halves[0], upper = halves[1];
+    const v2u a = __builtin_amdgcn_permlane16_swap(lower, lower, false, false);
+    const v2u b = __builtin_amdgcn_permlane16_swap(upper, upper, false, false);
+    of[0] = a[0], of[1] = a[1], of[2] = b[0], of[3] = b[1];
+}
+
+template <int GROUP, int NW, int NR>
+__global__ __launch_bounds__(NW *kWave) void w4a16_grouped_rows_kernel(const __half *__restrict__ X, int64_t ldx, int T, int K,
+                                                                       const uint8_t *__restrict__ Qw, const __half *__restrict__ steps,
+                                                                       int N, __half *__restrict__ Y, int64_t ldy)
+{
+    static_assert(NR % 2 == 0, "the token chunks alternate between two register sets");
+    constexpr int NT = NW * kWave, SUB = GROUP >= 128 ? 1 : 128 / GROUP, CHAIN = 4 / SUB;
+    constexpr int SPR = NR * 128 / GROUP, PIECE = SPR < 4 ? 1 : SPR / 4;       // steps per round, and of a quarter
+    constexpr int CHUNKS = (kMaxDynamicLds / 16 + NT - 1) / NT;                // 16-byte chunks of the rows per thread, at most
+    struct __attribute__((packed, aligned(2))) Piece {
+        unsigned short s[PIECE];
+    };
+    extern __shared__ uint4 rows_u4[];
+    char *xs = reinterpret_cast<char *>(rows_u4);
+    const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(tid / kWave);
+    const int l16 = lane & 15, q = lane >> 4;
+    const int stride = 2 * K + kRowPad, slices = K / 128, groups = K / GROUP, rounds = (slices + NR - 1) / NR;
+    const int blocks = (N + 15) / 16, mine = (blocks - (int)blockIdx.x + (int)gridDim.x - 1) / (int)gridDim.x;
+    // this wave's run: rounds [begin, end) of the workgroup's mine * rounds, numbered block after block
+    const int64_t all = (int64_t)mine * rounds;
+    const int begin = (int)(all * wave / NW), end = (int)(all * (wave + 1) / NW);
+    // Neighbouring workgroups begin their blocks with another round: the requests of a moment would meet in a few memory
+    // channels where rows of codes lie a multiple of 4 KB apart (T = 8, K = 8192, N = 28672, groups of 128: 33.4 -> 30.7 us),
+    // and elsewhere it costs nothing (T = 1, K = 11008, N = 57344: 69.7 -> 68.0).  The order of a channel's additions goes
+    // with it.
+    const int turn = (int)blockIdx.x % rounds;
+
+    // what is requested next; behind the run's end its last round again, dropped
+    auto channel = [&](int block) { return (int64_t)min(16 * ((int)blockIdx.x + block * (int)gridDim.x) + l16, N - 1); };
+    int ask = min(begin, (int)all - 1), ask_block = ask / rounds, ask_round;
+    const uint8_t *w_row;
+    const __half *s_row;
+    auto aim = [&]() {
+        const int r = ask - ask_block * rounds + turn;
+        ask_round = r >= rounds ? r - rounds : r;
+    };
+    auto aim_block = [&]() {
+        w_row = Qw + channel(ask_block) * (K / 2) + 16 * q;
+        s_row = steps + channel(ask_block) * groups;
+    };
+    aim();
+    aim_block();
+    auto advance = [&]() {
+        if (ask + 1 >= end) return;
+        ++ask;
+        if (ask == (ask_block + 1) * rounds) {
+            ++ask_block;
+            aim_block();
+        }
+        aim();
+    };
+    uint4 w[NR];
+    Piece s;                                           // of the round that is requested
+    auto ask_codes = [&](int k) { w[k] = *reinterpret_cast<const uint4 *>(w_row + min(NR * ask_round + k, slices - 1) * 64); };
+    auto ask_steps = [&]() {
+        const int at = ask_round * SPR + q * PIECE;
+        if (ask_round * SPR + 4 * PIECE <= groups) {
+            s = *reinterpret_cast<const Piece *>(s_row + at);
+        } else {
+#pragma unroll
+            for (int g = 0; g < PIECE; ++g) {
+                const unsigned short v = __half_as_ushort(s_row[min(at + g, groups - 1)]);
+                s.s[g] = at + g < groups ? v : 0;
+            }
+        }
+    };
+
+    // the token rows are requested first, then the first round; loads complete in order, so the rows go to LDS while the
+    // codes are on their way
+    const int chunks_per_row = K / 8, chunks = T * chunks_per_row;
+    {
+        uint4 xv[CHUNKS];
+#pragma unroll
+        for (int u = 0; u < CHUNKS; ++u) {
+            const int j = min(tid + NT * u, chunks - 1);
+            xv[u] = *reinterpret_cast<const uint4 *>(X + (int64_t)(j / chunks_per_row) * ldx + 8 * (j % chunks_per_row));
+        }
+        ask_steps();
+#pragma unroll
+        for (int k = 0; k < NR; ++k) ask_codes(k);
+#pragma unroll
+        for (int u = 0; u < CHUNKS; ++u) {
+            const int j = tid + NT * u;
+            if (j < chunks)
+                *reinterpret_cast<uint4 *>(xs + (j / chunks_per_row) * stride + 16 * (j % chunks_per_row)) = interleave_halves(xv[u]);
+        }
+    }
+    __syncthreads();
+
+    uint32_t magic;                                    // 1024.0 in both halves, held in a vector register
+    asm volatile("v_mov_b32 %0, 0x64006400" : "=v"(magic));
+    const char *xa = xs + min(l16, T - 1) * stride;    // rows past T repeat the last one: their products are never stored
+    v8h x[2][4];
+    auto read_tokens = [&](int set, int slice) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) x[set][j] = *reinterpret_cast<const v8h *>(xa + 256 * slice + 2 * slice_place<GROUP>(j, q));
+    };
+    // 16 x 16 accumulator layout: lane holds channel l16, register e holds token 4 q + e
+    auto store = [&](int block, const v4f &sum) {
+        const int n = 16 * ((int)blockIdx.x + block * (int)gridDim.x) + l16;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const int t = 4 * q + e;
+            if (t < T && n < N) Y[(int64_t)t * ldy + n] = __float2half_rn(sum[e]);
+        }
+    };
+    v4f total = {0.f, 0.f, 0.f, 0.f}, head = total;
+    int block = ask_block, round = ask_round, first_of_block = block * rounds;
+    read_tokens(0, round * NR);
+    advance();
+    for (int at = begin; at < end; ++at) {
+        const int next = round + 1 < rounds ? round + 1 : 0;          // behind a block's last round its first one, `turn`, again
+        uint32_t now[(PIECE + 1) / 2][4];                             // the steps of this round, two to a dword
+#pragma unroll
+        for (int g = 0; g < PIECE; g += 2) all_quarters(s.s[g] | (g + 1 < PIECE ? (uint32_t)s.s[g + 1 < PIECE ? g + 1 : g] << 16 : 0u), now[g / 2]);
+        ask_steps();
+#pragma unroll
+        for (int k = 0; k < NR; ++k) {
+            read_tokens((k + 1) & 1, k + 1 == NR ? next * NR : min(round * NR + k + 1, slices - 1));
+            uint32_t d[4] = {w[k].x, w[k].y, w[k].z, w[k].w};
+            sort_steps<GROUP>(d);
+#pragma unroll
+            for (int g = 0; g < SUB; ++g) {
+                v4f part = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int j = g * CHAIN; j < (g + 1) * CHAIN; ++j)
+                    part = __builtin_amdgcn_mfma_f32_16x16x32_f16(x[k & 1][j], widen_codes_f16(d[j], magic), part, 0, 0, 0);
+                const int step = k * SPR / NR + g, in = step % PIECE;          // of the round, of the quarter
+                const uint32_t pair = now[in / 2][step / PIECE];
+                const float f = __half2float(__ushort_as_half((unsigned short)(in % 2 ? pair >> 16 : pair)));
+#pragma unroll
+                for (int e = 0; e < 4; ++e) total[e] = __builtin_fmaf(f, part[e], total[e]);
+            }
+            ask_codes(k);
+            // keep the requests here, one slice behind another: collected at the end of the round they would be waited for at once
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        advance();
+        round = next;
+        if (at + 1 == first_of_block + rounds) {
+            if (first_of_block >= begin)
+                store(block, total);
+            else
+                head = total;
+            total = v4f{0.f, 0.f, 0.f, 0.f};
+            ++block;
+            first_of_block += rounds;
+        }
+    }
+    // A run's last block, if it goes on in the next waves' runs: the rest of it is their `head`, or all of their sum where
+    // it does not end there either.
+    const bool begun = first_of_block >= begin && first_of_block < end;
+    if (first_of_block < begin && begin < end) head = total;
+    v4f *heads = reinterpret_cast<v4f *>(rows_u4);
+    __syncthreads();                                   // all are done with the rows
+    heads[wave * kWave + lane] = head;
+    __syncthreads();
+    if (!begun) return;
+    for (int v = wave + 1; v < NW && (int)(all * v / NW) < first_of_block + rounds; ++v) {
+        const v4f more = heads[v * kWave + lane];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) total[e] += more[e];
+    }
+    store(block, total);
 }
 
 struct GroupedArgs {
@@ -196,19 +386,36 @@ struct GroupedArgs {
     hipStream_t st;
 };
 
-template <int GROUP, int NS, int NW, int TT, int D>
+template <int GROUP, int NS, int NW, int TT, int H>
 sq_status launch_grouped_skinny(const GroupedArgs &a)
 {
-    hipLaunchKernelGGL((w4a16_grouped_skinny_kernel<GROUP, NS, NW, TT, D>), dim3((unsigned)((a.N + 16 * NS - 1) / (16 * NS))), dim3(NW * kWave),
-                       0, a.st, a.X, a.ldx, a.T, a.K, a.Qw, a.steps, a.group, a.N, a.Y, a.ldy);
+    hipLaunchKernelGGL((w4a16_grouped_skinny_kernel<GROUP, NS, NW, TT, H>),
+                       dim3((unsigned)((a.N + 16 * NS - 1) / (16 * NS)), (unsigned)((a.T + 16 * TT - 1) / (16 * TT))), dim3(NW * kWave), 0, a.st,
+                       a.X, a.ldx, a.T, a.K, a.Qw, a.steps, a.N, a.Y, a.ldy);
+    return hipGetLastError() == hipSuccess ? SQ_OK : SQ_ERR_LAUNCH;
+}
+
+template <int GROUP, int NW, int NR>
+sq_status launch_grouped_rows(const GroupedArgs &a)
+{
+    const int blocks = (a.N + 15) / 16, grid = blocks < 256 ? blocks : 256;
+    auto kernel = w4a16_grouped_rows_kernel<GROUP, NW, NR>;
+    if (!allow_large_lds(reinterpret_cast<const void *>(kernel))) return SQ_ERR_LAUNCH;
+    const size_t rows = (size_t)a.T * (2 * a.K + kRowPad), heads = (size_t)NW * kWave * 16;
+    hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(NW * kWave), rows > heads ? rows : heads, a.st, a.X, a.ldx, a.T, a.K, a.Qw, a.steps, a.N,
+                       a.Y, a.ldy);
     return hipGetLastError() == hipSuccess ? SQ_OK : SQ_ERR_LAUNCH;
 }
 
 template <int GROUP>
 sq_status launch_grouped_few(const GroupedArgs &a)
 {
-    if (a.T > 16) return launch_grouped_skinny<GROUP, 1, 8, 2, 2>(a);
-    if (a.N >= 16384) return launch_grouped_skinny<GROUP, 2, 4, 1, 2>(a);
+    if (a.T <= 16 && a.K % 128 == 0 && a.T * (int64_t)(2 * a.K + kRowPad) <= kMaxDynamicLds && (int64_t)a.K * a.N >= ((int64_t)32 << 20))
+        return launch_grouped_rows<GROUP, 8, 4>(a);
+    const int tiles = (a.T + 15) / 16, blocks = (a.N + 15) / 16;
+    if (tiles == 2 && blocks / 4 >= 170) return launch_grouped_skinny<GROUP, 4, 8, 2, 1>(a);
+    if (blocks / 4 * tiles >= 170) return launch_grouped_skinny<GROUP, 4, 8, 1, GROUP <= 64 ? 1 : 2>(a);
+    if (blocks / 2 * tiles >= 170) return launch_grouped_skinny<GROUP, 2, 8, 1, 2>(a);
     return launch_grouped_skinny<GROUP, 1, 8, 1, 2>(a);
 }
 
@@ -258,7 +465,8 @@ extern "C" sq_status sq_w4a16_gemm_grouped(const void *X, int64_t T, int32_t K, 
                                    static_cast<__half *>(Y), ldy, static_cast<hipStream_t>(stream)};
         if (group == 32) return sq::launch_grouped_few<32>(a);
         if (group == 64) return sq::launch_grouped_few<64>(a);
-        return sq::launch_grouped_few<128>(a);
+        if (group == 128) return sq::launch_grouped_few<128>(a);
+        return sq::launch_grouped_few<256>(a);
     }
     const int64_t blocks = (T * N + 3) / 4;
     if (blocks > 0x7FFFFFFF) return SQ_ERR_SHAPE;
