@@ -419,31 +419,19 @@ sq_status launch_grouped_few(const GroupedArgs &a)
     return launch_grouped_skinny<GROUP, 1, 8, 1, 2>(a);
 }
 
-// One wave per output: a lane takes every 64th run of eight codes, multiplies in fp32 and adds its sum times the group's
-// step; the lanes' sums are added at the end.
-__global__ __launch_bounds__(256) void w4a16_grouped_dot_kernel(const __half *__restrict__ X, int64_t ldx, int T, int K,
-                                                                const uint8_t *__restrict__ Qw, const __half *__restrict__ steps,
-                                                                int group, int N, __half *__restrict__ Y, int64_t ldy)
+// Many tokens: the tile kernel of sq_w4a16_gemm with the steps on the widened codes, in its shapes and by its rules.
+sq_status launch_grouped_many(const GroupedArgs &a)
 {
-    const int lane = threadIdx.x & (kWave - 1);
-    const int64_t id = (int64_t)blockIdx.x * 4 + threadIdx.x / kWave;
-    const int64_t t = id / N;
-    const int n = (int)(id - t * N);
-    if (t >= T) return;
-    const uint32_t *q = reinterpret_cast<const uint32_t *>(Qw + (int64_t)n * (K / 2));
-    const __half *s = steps + (int64_t)n * (K / group), *x = X + t * ldx;
-    float sum = 0.f;
-    for (int u = lane; u < K / 8; u += kWave) {
-        const uint32_t w = q[u];
-        const v8h a = *reinterpret_cast<const v8h *>(x + 8 * u);
-        float part = 0.f;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) part = __builtin_fmaf((float)a[e], (float)((int32_t)(w << (28 - 4 * e)) >> 28), part);
-        sum = __builtin_fmaf(part, __half2float(s[8 * u / group]), sum);
-    }
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o, kWave);
-    if (lane == 0) Y[t * ldy + n] = __float2half_rn(sum);
+    const int shift = __builtin_ctz((unsigned)a.group);
+    const int64_t tiles_64x128 = ((int64_t)a.T + 63) / 64 * (((int64_t)a.N + 127) / 128), tiles_128 = ((int64_t)a.T + 127) / 128 * (((int64_t)a.N + 127) / 128);
+    const int64_t tiles_large = ((int64_t)a.T + 255) / 256 * (((int64_t)a.N + 255) / 256);
+    if (a.K % 128 == 0 && tiles_64x128 <= 256)
+        return launch_w4a16_ring<1, 4, 2, 1, 1, 64, 0, 2, true>(a.X, a.ldx, a.T, a.K, a.Qw, a.steps, a.N, a.Y, a.ldy, a.st, shift);
+    if (a.K % 128 == 0 && tiles_128 <= 256)
+        return launch_w4a16_ring<1, 4, 4, 1, 1, 64, 0, 2, true>(a.X, a.ldx, a.T, a.K, a.Qw, a.steps, a.N, a.Y, a.ldy, a.st, shift);
+    if (tiles_large >= 192)
+        return launch_w4a16_ring<2, 4, 4, 2, 1, 64, 0, 1, true>(a.X, a.ldx, a.T, a.K, a.Qw, a.steps, a.N, a.Y, a.ldy, a.st, shift);
+    return launch_w4a16_ring<1, 4, 4, 2, 1, 64, 4, 1, true>(a.X, a.ldx, a.T, a.K, a.Qw, a.steps, a.N, a.Y, a.ldy, a.st, shift);
 }
 
 }  // namespace
@@ -460,18 +448,11 @@ extern "C" sq_status sq_w4a16_gemm_grouped(const void *X, int64_t T, int32_t K, 
     if (!X || !Qw || !steps || !Y) return SQ_ERR_NULL;
     if (((uintptr_t)X & 15) || (ldx % 8) != 0 || ((uintptr_t)Qw & 15) || ((uintptr_t)Y & 1) || ((uintptr_t)steps & 1))
         return SQ_ERR_ALIGN;
-    if (T <= 32) {
-        const sq::GroupedArgs a = {static_cast<const __half *>(X), ldx, (int)T, K, Qw, static_cast<const __half *>(steps), group, N,
-                                   static_cast<__half *>(Y), ldy, static_cast<hipStream_t>(stream)};
-        if (group == 32) return sq::launch_grouped_few<32>(a);
-        if (group == 64) return sq::launch_grouped_few<64>(a);
-        if (group == 128) return sq::launch_grouped_few<128>(a);
-        return sq::launch_grouped_few<256>(a);
-    }
-    const int64_t blocks = (T * N + 3) / 4;
-    if (blocks > 0x7FFFFFFF) return SQ_ERR_SHAPE;
-    hipLaunchKernelGGL(sq::w4a16_grouped_dot_kernel, dim3((unsigned)blocks), dim3(256), 0, static_cast<hipStream_t>(stream),
-                       static_cast<const __half *>(X), ldx, (int)T, K, Qw, static_cast<const __half *>(steps), group, N,
-                       static_cast<__half *>(Y), ldy);
-    return hipGetLastError() == hipSuccess ? SQ_OK : SQ_ERR_LAUNCH;
+    const sq::GroupedArgs a = {static_cast<const __half *>(X), ldx, (int)T, K, Qw, static_cast<const __half *>(steps), group, N,
+                               static_cast<__half *>(Y), ldy, static_cast<hipStream_t>(stream)};
+    if (T > 32) return sq::launch_grouped_many(a);
+    if (group == 32) return sq::launch_grouped_few<32>(a);
+    if (group == 64) return sq::launch_grouped_few<64>(a);
+    if (group == 128) return sq::launch_grouped_few<128>(a);
+    return sq::launch_grouped_few<256>(a);
 }

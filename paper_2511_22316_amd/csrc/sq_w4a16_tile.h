@@ -3,6 +3,8 @@
 
 #include "sq_gemm_tile.h"
 
+#include <type_traits>
+
 namespace sq {
 
 namespace {
@@ -82,6 +84,20 @@ __device__ __forceinline__ void dma_16_if(const void *gptr, uint32_t lds_addr, i
                  : "memory", "m0", "scc");
 }
 
+__device__ __forceinline__ void dma_2_if(const void *gptr, uint32_t lds_addr, int a, int b)
+{
+    // two bytes per lane, global memory -> the dword at lds_addr + 4 lane, zero-extended; else as dma_16_if
+    asm volatile("s_cmp_lt_i32 %2, %3\n\t"
+                 "s_cbranch_scc0 .Lsq2_skip_%=\n\t"
+                 "s_mov_b32 m0, %1\n\t"
+                 "s_nop 0\n\t"
+                 "global_load_lds_ushort %0, off\n"
+                 ".Lsq2_skip_%=:"
+                 :
+                 : "v"(gptr), "s"(lds_addr), "s"(a), "s"(b)
+                 : "memory", "m0", "scc");
+}
+
 // Tile kernel for many tokens.  Block tile (WM FM 32) tokens x (WN FN 32) channels, WM x WN waves
 // of FM x FN fragments of 32 x 32; K walked in tiles of 64.  Both operands travel global -> LDS
 // without passing registers (16 bytes per lane), through a ring of three stages, two tiles ahead,
@@ -108,11 +124,15 @@ __device__ __forceinline__ void dma_16_if(const void *gptr, uint32_t lds_addr, i
 // LW > 0: LW more waves that only request the tiles and wait for them; the multiplying waves then
 // issue no memory instruction inside the loop and meet the others at the barrier of each tile.
 // KG: groups of WM WN waves that walk K / KG elements each, through rings of their own, and add their sums through LDS.
-template <int WM, int WN, int FM, int FN, int OCC, int BK, int LW, int KG>
+// GROUPED: a step per group of 1 << group_shift >= 32 elements of K in place of one per channel.  The steps of a tile's two
+// halves travel with it (a dword each), and a widened code is multiplied by its step in fp16, rounded once: a lane's 32
+// elements of a tile lie in one group, so that is one packed multiplication per two codes (four widening instructions
+// instead of three).  Scaling the sums instead would keep them exact, but wants as many registers again as the sums have.
+template <int WM, int WN, int FM, int FN, int OCC, int BK, int LW, int KG, bool GROUPED>
 __global__ __launch_bounds__((KG * WM * WN + LW) * kWave, OCC) void w4a16_gemm_ring_kernel(
     const __half *__restrict__ X, int64_t ldx, int T, int K, const uint8_t *__restrict__ Qw,
-    const float *__restrict__ sw, int N, __half *__restrict__ Y, int64_t ldy, int tiles_m, int tiles_n,
-    int vec_store)
+    const typename std::conditional<GROUPED, __half, float>::type *__restrict__ sw, int N, __half *__restrict__ Y, int64_t ldy,
+    int tiles_m, int tiles_n, int vec_store, int group_shift)
 {
     static_assert(BK == 64, "tiles of 64 elements of K");
     constexpr int NW = WM * WN, NS = 3, STEPS = BK / 16;     // waves of a group; ring stages; MFMA steps per K tile
@@ -121,11 +141,14 @@ __global__ __launch_bounds__((KG * WM * WN + LW) * kWave, OCC) void w4a16_gemm_r
     constexpr int A_ROW = 2 * BK, B_ROW = BK / 2;            // bytes of a tile row
     constexpr int A_CPR = A_ROW / 16, B_CPR = B_ROW / 16;    // 16-byte chunks per row
     constexpr int A_RPL = 64 / A_CPR, B_RPL = 64 / B_CPR;    // rows filled by one wave-wide load
-    constexpr int A_BYTES = BM * A_ROW, B_BYTES = BN * B_ROW, STAGE = A_BYTES + B_BYTES;
+    constexpr int A_BYTES = BM * A_ROW, B_BYTES = BN * B_ROW, S_BYTES = GROUPED ? 2 * BN * 4 : 0;
+    constexpr int STAGE = A_BYTES + B_BYTES + S_BYTES;
     constexpr int NL = LW > 0 ? LW : NW;                     // waves that share the loads of a tile
     constexpr int A_LOADS = BM / A_RPL / NL, B_LOADS = BN / B_RPL / NL;       // wave-wide loads per loading wave and tile
-    constexpr int LOADS = A_LOADS + B_LOADS;
-    static_assert((BM / A_RPL) % NL == 0 && (BN / B_RPL) % NL == 0, "loads must split evenly over the waves");
+    constexpr int S_LOADS = GROUPED ? 2 * BN / kWave / NL : 0;
+    constexpr int LOADS = A_LOADS + B_LOADS + S_LOADS;
+    static_assert((BM / A_RPL) % NL == 0 && (BN / B_RPL) % NL == 0 && (!GROUPED || 2 * BN / kWave % NL == 0),
+                  "loads must split evenly over the waves");
     extern __shared__ uint4 ring[];
 
     const int tid = threadIdx.x, lane = tid & (kWave - 1);
@@ -163,6 +186,13 @@ __global__ __launch_bounds__((KG * WM * WN + LW) * kWave, OCC) void w4a16_gemm_r
         const int r = B_RPL * (wave + NL * u) + lane / B_CPR;
         b_src[u] = Qw + (int64_t)min(col0 + r, N - 1) * Kb + kg0 / 2 + (lane % B_CPR) * 16;
     }
+    // steps: entry BN half + channel; 64 neighbouring ones are of one half
+    const __half *s_src[GROUPED ? S_LOADS : 1];
+    if constexpr (GROUPED) {
+#pragma unroll
+        for (int u = 0; u < S_LOADS; ++u)
+            s_src[u] = sw + (int64_t)min(col0 + (kWave * (wave + NL * u) + lane) % BN, N - 1) * (K >> group_shift);
+    }
     const uint32_t lds_base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint4 *)ring + kg * (NS * STAGE);
     const uint32_t wave_u = __builtin_amdgcn_readfirstlane(wave);
     auto issue_tile = [&](int kt, int stage, int limit) {
@@ -172,6 +202,14 @@ __global__ __launch_bounds__((KG * WM * WN + LW) * kWave, OCC) void w4a16_gemm_r
 #pragma unroll
         for (int u = 0; u < B_LOADS; ++u)
             dma_16_if(b_src[u] + kt * (BK / 2), sa + A_BYTES + (wave_u + NL * u) * 1024, kt, limit);
+        if constexpr (GROUPED) {
+#pragma unroll
+            for (int u = 0; u < S_LOADS; ++u) {
+                const int half = kWave * ((int)wave_u + NL * u) / BN;
+                dma_2_if(s_src[u] + ((kg0 + min(kt, limit - 1) * BK + half * (BK / 2)) >> group_shift),
+                         sa + A_BYTES + B_BYTES + (wave_u + NL * u) * (4 * kWave), kt, limit);
+            }
+        }
     };
 
     v16f acc[FM][FN];
@@ -189,6 +227,7 @@ __global__ __launch_bounds__((KG * WM * WN + LW) * kWave, OCC) void w4a16_gemm_r
     for (int s = 0; s < STEPS; ++s)
         a_off[s] = (wm * FM * 32 + l32) * A_ROW + (((STEPS * g + s) ^ ((l32 >> 1) & 7)) * 16);
     const int b_off = A_BYTES + (wn * FN * 32 + l32) * B_ROW + g * (STEPS * 4);
+    const int s_off = A_BYTES + B_BYTES + (g * BN + wn * FN * 32 + l32) * 4;
     const char *lds = reinterpret_cast<const char *>(ring) + kg * (NS * STAGE);
 
     uint32_t magic;                                    // 1024.0 in both halves, held in a vector register
@@ -224,10 +263,14 @@ __global__ __launch_bounds__((KG * WM * WN + LW) * kWave, OCC) void w4a16_gemm_r
     uint4 rb[FN];
     v8h a[2][FM];
     v4u b[2][FN];
-    uint32_t flipped[FN];
+    uint32_t flipped[FN], step2[GROUPED ? FN : 1];     // step2: the step of this lane's half of the tile, twice
     auto read_codes = [&](int stage_byte) {
 #pragma unroll
         for (int j = 0; j < FN; ++j) rb[j] = *reinterpret_cast<const uint4 *>(lds + stage_byte + b_off + j * (32 * B_ROW));
+        if constexpr (GROUPED) {
+#pragma unroll
+            for (int j = 0; j < FN; ++j) step2[j] = *reinterpret_cast<const uint32_t *>(lds + stage_byte + s_off + j * (32 * 4)) * 0x10001u;
+        }
     };
     auto read_tokens = [&](int set, int stage_byte, int s, int i) {
         a[set][i] = *reinterpret_cast<const v8h *>(lds + stage_byte + a_off[s] + i * (32 * A_ROW));
@@ -240,6 +283,10 @@ __global__ __launch_bounds__((KG * WM * WN + LW) * kWave, OCC) void w4a16_gemm_r
                            : u % 4 == 1 ? widen_byte_f16<1>(flipped[j], magic)
                            : u % 4 == 2 ? widen_byte_f16<2>(flipped[j], magic)
                                         : widen_byte_f16<3>(flipped[j], magic);
+        if constexpr (GROUPED) {
+            const uint32_t code2 = b[set][j][u % 4];
+            b[set][j][u % 4] = __builtin_bit_cast(uint32_t, __builtin_bit_cast(v2h, code2) * __builtin_bit_cast(v2h, step2[j]));
+        }
     };
     // One step on set C; the next one's operands are step S of the tile at BYTE.  TURN: the turn into that tile comes
     // first, and its codes are read; they are widened in the second half of the step.
@@ -323,7 +370,12 @@ __global__ __launch_bounds__((KG * WM * WN + LW) * kWave, OCC) void w4a16_gemm_r
 #pragma unroll
         for (int q = 0; q < 4; ++q)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) swq[q][r] = sw[min(nf + 8 * q + 4 * g + r, N - 1)];
+            for (int r = 0; r < 4; ++r) {
+                if constexpr (GROUPED)
+                    swq[q][r] = 1.f;
+                else
+                    swq[q][r] = sw[min(nf + 8 * q + 4 * g + r, N - 1)];
+            }
 #pragma unroll
         for (int i = 0; i < FM; ++i) {
             const int t = row0 + (wm * FM + i) * 32 + l32;
@@ -359,20 +411,21 @@ __global__ __launch_bounds__((KG * WM * WN + LW) * kWave, OCC) void w4a16_gemm_r
     }
 }
 
-template <int WM, int WN, int FM, int FN, int OCC, int BK, int LW = 0, int KG = 1>
-sq_status launch_w4a16_ring(const __half *X, int64_t ldx, int T, int K, const uint8_t *Qw, const float *sw, int N,
-                            __half *Y, int64_t ldy, hipStream_t st)
+template <int WM, int WN, int FM, int FN, int OCC, int BK, int LW = 0, int KG = 1, bool GROUPED = false>
+sq_status launch_w4a16_ring(const __half *X, int64_t ldx, int T, int K, const uint8_t *Qw,
+                            const typename std::conditional<GROUPED, __half, float>::type *sw, int N, __half *Y, int64_t ldy, hipStream_t st,
+                            int group_shift = 0)
 {
     constexpr int BM = WM * FM * 32, BN = WN * FN * 32;
-    constexpr size_t lds = (size_t)3 * KG * (BM * 2 * BK + BN * BK / 2);
+    constexpr size_t lds = (size_t)3 * KG * (BM * 2 * BK + BN * BK / 2 + (GROUPED ? 2 * BN * 4 : 0));
     static_assert(lds <= (size_t)kMaxDynamicLds, "ring does not fit in LDS");
-    auto kernel = w4a16_gemm_ring_kernel<WM, WN, FM, FN, OCC, BK, LW, KG>;
+    auto kernel = w4a16_gemm_ring_kernel<WM, WN, FM, FN, OCC, BK, LW, KG, GROUPED>;
     if ((K % (KG * BK)) != 0) return SQ_ERR_SHAPE;
     if (!allow_large_lds(reinterpret_cast<const void *>(kernel))) return SQ_ERR_LAUNCH;
     const int tiles_m = (T + BM - 1) / BM, tiles_n = (N + BN - 1) / BN;
     const int vec_store = (((uintptr_t)Y & 15) == 0 && (ldy % 8) == 0) ? 1 : 0;
     hipLaunchKernelGGL(kernel, dim3((unsigned)(tiles_m * tiles_n)), dim3((KG * WM * WN + LW) * kWave), lds, st, X, ldx, T, K, Qw,
-                       sw, N, Y, ldy, tiles_m, tiles_n, vec_store);
+                       sw, N, Y, ldy, tiles_m, tiles_n, vec_store, group_shift);
     return hipGetLastError() == hipSuccess ? SQ_OK : SQ_ERR_LAUNCH;
 }
 

@@ -106,7 +106,8 @@ FEW = [(1, 64, 1, 32), (1, 64, 17, 64), (1, 256, 100, 256), (2, 320, 33, 64), (3
        (16, 4096, 130, 32), (15, 2048, 16, 64), (5, 11008, 48, 128), (17, 512, 96, 32), (32, 1024, 80, 256), (31, 4160, 40, 32),
        (8, 8192, 4100, 128), (1, 8192, 4112, 32), (4, 1024, 16500, 64), (1, 28672, 64, 64), (7, 192, 20000, 32), (1, 131072, 20, 256)]
 MANY = [(33, 64, 40, 32), (64, 4096, 256, 128), (100, 320, 130, 64), (333, 512, 200, 32), (129, 2048, 97, 256), (257, 1088, 64, 64),
-        (600, 4096, 300, 32), (1000, 256, 1111, 128), (2048, 128, 512, 64)]
+        (600, 4096, 300, 32), (1000, 256, 1111, 128), (2048, 128, 512, 64),
+        (3300, 192, 3900, 64), (3300, 256, 3850, 32)]
 
 
 @pytest.mark.parametrize("T,K,N,group", FEW + MANY)
