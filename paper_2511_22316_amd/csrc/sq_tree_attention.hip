@@ -9,6 +9,7 @@ namespace {
 constexpr int kKeysPerTile = 32;       // of one wave and step
 constexpr int kWaves = 4;
 constexpr int kChunkUnit = kKeysPerTile * kWaves;
+constexpr int kMaxSplits = 64;         // a lane each in the kernel that joins them
 constexpr float kNothing = -1e30f;     // running maximum of a row that has seen no key
 
 // Four fp16 of one dword pair.
@@ -371,21 +372,27 @@ __global__ __launch_bounds__(kWaves *kWave, D == 256 ? 2 : R == 1 ? 4 : 2) void 
     }
 }
 
-// The splits of a row and head: one wave, a lane D / 64 channels.  The shares of the splits (at most 64) are worked out
-// one to a lane.
+// The splits of a row and head, at most kMaxSplits: one workgroup, D / 4 threads to a split, so that all sums are requested at
+// once.  (One wave walking over the splits took 17.7 us for 64 of them.)
 template <int D>
 __global__ __launch_bounds__(256) void tree_attention_join_kernel(const CacheView c, const AttentionCall a)
 {
-    constexpr int PER = D / 64;
-    const int lane = threadIdx.x & (kWave - 1);
-    const int b = blockIdx.y;
-    const int64_t unit = (int64_t)blockIdx.x * 4 + threadIdx.x / kWave;
-    const int64_t i = unit / a.Hq, hq = unit - i * a.Hq;
+    constexpr int LANES = D / 4, SIDE = 256 / LANES, MOST = kMaxSplits / SIDE;     // threads of a split; splits side by side; rounds of them
+    __shared__ float shares[kMaxSplits], totals;
+    __shared__ float4 sums[SIDE][LANES];
+    const int tid = threadIdx.x, lane = tid & (kWave - 1), mine = tid % LANES, side = tid / LANES;
+    const int b = blockIdx.y, i = (int)(blockIdx.x / (unsigned)a.Hq), hq = (int)(blockIdx.x % (unsigned)a.Hq);
     int64_t first;
     const int n = rows_of(c, a, b, first);
     if (i >= min(n, a.max_rows)) return;
     const int64_t place = ((first + i) * a.Hq + hq) * a.splits;
     const float2 ml = reinterpret_cast<const float2 *>(a.part + a.T * a.Hq * (int64_t)a.splits * D)[place + min(lane, a.splits - 1)];
+    float4 v[MOST];
+#pragma unroll
+    for (int k = 0; k < MOST; ++k) {
+        v[k] = float4{0.f, 0.f, 0.f, 0.f};
+        if (k * SIDE < a.splits) v[k] = reinterpret_cast<const float4 *>(a.part + (place + min(k * SIDE + side, a.splits - 1)) * D)[mine];
+    }
     const bool there = lane < a.splits && ml.y > 0.f;
     float top = there ? ml.x : kNothing;
 #pragma unroll
@@ -394,16 +401,30 @@ __global__ __launch_bounds__(256) void tree_attention_join_kernel(const CacheVie
     float total = share * (there ? ml.y : 0.f);
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) total += __shfl_xor(total, o, kWave);
-    float out[PER] = {};
-    const float *src = a.part + place * D + PER * lane;
-    for (int s = 0; s < a.splits; ++s) {
-        const float w = __shfl(share, s, kWave);
-#pragma unroll
-        for (int k = 0; k < PER; ++k) out[k] = __builtin_fmaf(w, src[(int64_t)s * D + k], out[k]);
+    if (tid < kWave) {
+        shares[lane] = share;                              // 0 behind the last split
+        if (lane == 0) totals = total;
     }
-    const float scale = total > 0.f ? 1.f / total : 0.f;
+    __syncthreads();
+    float4 sum = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int k = 0; k < PER; ++k) a.O[(first + i) * a.ldo + hq * D + PER * lane + k] = __float2half_rn(out[k] * scale);
+    for (int k = 0; k < MOST; ++k) {
+        if (k * SIDE >= a.splits) break;
+        const float w = shares[k * SIDE + side];
+        sum.x = __builtin_fmaf(w, v[k].x, sum.x), sum.y = __builtin_fmaf(w, v[k].y, sum.y);
+        sum.z = __builtin_fmaf(w, v[k].z, sum.z), sum.w = __builtin_fmaf(w, v[k].w, sum.w);
+    }
+    sums[side][mine] = sum;
+    __syncthreads();
+    if (tid >= LANES) return;
+#pragma unroll
+    for (int k = 1; k < SIDE; ++k) {
+        const float4 x = sums[k][mine];
+        sum.x += x.x, sum.y += x.y, sum.z += x.z, sum.w += x.w;
+    }
+    const float scale = totals > 0.f ? 1.f / totals : 0.f;
+    const v4hs y = {(_Float16)(sum.x * scale), (_Float16)(sum.y * scale), (_Float16)(sum.z * scale), (_Float16)(sum.w * scale)};
+    *reinterpret_cast<v4hs *>(a.O + (first + i) * a.ldo + hq * D + 4 * mine) = y;
 }
 
 template <int D, int R>
@@ -415,7 +436,8 @@ sq_status launch_tree_attention(const CacheView &c, const AttentionCall &a, hipS
     if (hipGetLastError() != hipSuccess) return SQ_ERR_LAUNCH;
     if (a.splits == 1) return SQ_OK;
     const int64_t units = (int64_t)a.max_rows * a.Hq;
-    hipLaunchKernelGGL(tree_attention_join_kernel<D>, dim3((unsigned)((units + 3) / 4), (unsigned)c.B), dim3(256), 0, st, c, a);
+    if (units > 0x7FFFFFFF) return SQ_ERR_SHAPE;
+    hipLaunchKernelGGL(tree_attention_join_kernel<D>, dim3((unsigned)units, (unsigned)c.B), dim3(256), 0, st, c, a);
     return hipGetLastError() == hipSuccess ? SQ_OK : SQ_ERR_LAUNCH;
 }
 
@@ -433,7 +455,7 @@ sq_status dispatch_tree_attention(const CacheView &c, AttentionCall &a, int64_t 
     int64_t splits = (1024 + units - 1) / units;
     const int64_t chunks = (max_keys + kChunkUnit - 1) / kChunkUnit, room = workspace_bytes / (a.T * a.Hq * (D + 2) * 4);
     splits = splits < chunks ? splits : chunks;
-    splits = splits < 64 ? splits : 64;
+    splits = splits < kMaxSplits ? splits : kMaxSplits;
     splits = splits < room ? splits : room;
     a.splits = splits < 1 ? 1 : (int)splits;
     a.part = static_cast<float *>(workspace);
