@@ -569,7 +569,7 @@ sq_status sq_cache_read(const void *cache, int32_t pages, int32_t Hk, int32_t D,
  *              out: their rows of O keep what they held); <= 64 with a mask
  *   max_keys   about the longest cached[b] + new rows: how finely the work is split.
  *              Any value gives the right result.
- *   scale      > 0
+ *   scale      in (0, 1e20); scores scale * Q . k beyond 2^26 are not told apart
  *   workspace  device, 16-byte aligned, workspace_bytes long, or NULL and 0.  The sums
  *              of a split sequence meet in it; with less than
  *              sq_tree_attention_workspace_bytes the work is split less.  Nothing in

@@ -1,7 +1,9 @@
 // sq_tree_attention: attention of new rows (one token a sequence, a tree of drafted tokens, or a prompt) over the paged
 // 4-bit cache that holds them and everything before them.
 #include "sq_cache.h"
+#include "sq_gemm_tile.h"
 
+#include <type_traits>
 namespace sq {
 
 namespace {
@@ -27,6 +29,20 @@ __device__ __forceinline__ float quarter_max(float v)
     const uint32_t t0 = t[0], t1 = t[1];
     return fmaxf(__builtin_bit_cast(float, t0), __builtin_bit_cast(float, t1));
 }
+// 16 (or 4) bytes per lane, global memory base + offset -> LDS at lds_addr + 16 (4) lane
+__device__ __forceinline__ void dma_16(const uint8_t *base, uint32_t offset, uint32_t lds_addr)
+{
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" : : "v"(offset), "s"(base), "s"(lds_addr) : "memory", "m0");
+}
+__device__ __forceinline__ void dma_16(const uint8_t *lane_at, uint32_t lds_addr)
+{
+    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" : : "v"(lane_at), "s"(lds_addr) : "memory", "m0");
+}
+__device__ __forceinline__ void dma_4(const uint8_t *lane_at, uint32_t lds_addr)
+{
+    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %0, off" : : "v"(lane_at), "s"(lds_addr) : "memory", "m0");
+}
+
 __device__ __forceinline__ float quarter_sum(float v)
 {
     v += __shfl_xor(v, 16, kWave);
@@ -41,7 +57,7 @@ struct AttentionCall {
     float *part;               // [T, Hq, splits, D] sums of a split, then [T, Hq, splits] (maximum, sum); null: one split
     int64_t ldq, ldo, T;
     int Hq, group, max_rows, splits, row_blocks, tiles_per_chunk;
-    float score_scale;         // scale * log2(e) * 2^18
+    float score_scale;         // scale * log2(e) * 2^20
 };
 
 // New rows of sequence b that the call has: their number, and the first.
@@ -53,7 +69,7 @@ __device__ __forceinline__ int rows_of(const CacheView &c, const AttentionCall &
     return (int)max((int64_t)0, n);
 }
 
-// A workgroup takes one head of K and V of one sequence, 16 R query rows (row = new row * group + query head in the group)
+// A workgroup takes one head of K and V of one sequence, 16 query rows (row = new row * group + query head in the group)
 // and every splits-th chunk of its keys; its four waves take every fourth tile of 32 keys each and work alone until
 // the end.
 //
@@ -62,28 +78,34 @@ __device__ __forceinline__ int rows_of(const CacheView &c, const AttentionCall &
 // already the other operand of O^T = V^T P, whose contraction runs over the keys: nothing is moved between lanes but
 // the maximum (two swaps).  O^T again has the query row in the lane.
 //
-// Nibbles (code + 8) become fp16 without a conversion: a nibble in bits 6 to 9 of a half is the subnormal u 2^-18, which
+// Nibbles (code + 8) become fp16 without a conversion: a nibble in bits 4 to 7 of a half is the subnormal u 2^-20, which
 // the matrix cores take as it is.  (They line products up by the exponents alone: a subnormal counts as 2^-14, so the low
-// bits that its leading zeros push out are lost.  In bits 0 to 3 the same sums were off by 2^-14 of a step, in bits 6 to
-// 9 it is 2^-20.)  For K a dword gives four pairs, one shift and one and each; V's pairs need the same channel of two keys,
-// which one byte permute brings together for two channels.  The eights come off by sums: the scores' accumulators start at
-// -8 * 2^-18 * sum(q), and a matrix instruction with ones in place of V gives the sum of the weights.
+// bits that its leading zeros push out are lost.  In bits 0 to 3 the sums of a few keys were off by 2^-14 of a step, in
+// bits 4 to 7 it is 2^-18; in long sums the accumulator's own exponent decides.)  For K a dword gives four pairs, an and
+// and at most one shift each; V's pairs need the same channel of two keys, which one byte permute brings together for two
+// channels.  The eights come off by sums: the scores' accumulators start at -8 * 2^-20 * sum(q), and a matrix instruction
+// with ones in place of V gives the sum of the weights.
 //
 // Softmax with a running offset M per row: a weight is exp2(s - M) times the value's step, rounded to fp16 (its half step
 // of rounding averages out over the keys; the normaliser keeps the weight in fp32).  M goes by the largest of score plus
-// exponent of the step, so the largest product lies between 2^-1 and 2^6 whatever the steps are, and moves only when
-// that is passed.
+// logarithm of the step, so the largest product lies between 2^-1 and 2^7 whatever the steps are, and moves only when
+// that is passed.  The logarithm is the step's fp32 bits taken as a number, which is right to 0.09.
 //
-// Loads: K of the next tile is requested when this one's scores are done, V when its products are: one set of registers,
-// all of it in flight most of the time.
-template <int D, int R>
-__global__ __launch_bounds__(kWaves *kWave, D == 256 ? 2 : R == 1 ? 4 : 2) void tree_attention_kernel(const CacheView c, const AttentionCall a)
+// Loads: global memory -> LDS, two stages per wave; a tile goes to registers as soon as it has landed, and its stage is
+// requested again in front of the work on it, so two tiles are in flight all the time.  A wave waits for its own requests
+// only.  The page numbers are requested a tile ahead of that.
+// ONE_PAGE: pages of 32 rows and more, a tile lies in one.
+template <int D, bool ONE_PAGE>
+__global__ __launch_bounds__(kWaves *kWave, D == 256 ? 2 : 4) void tree_attention_kernel(const CacheView c, const AttentionCall a)
 {
     constexpr int KD = D / 32;                       // dwords of K (and of V) per lane and 16 keys; steps of the scores
     constexpr int VT = D / 16;                       // 16-channel tiles of the output
     constexpr int CB = D < 128 ? D : 128, LD = CB + 4;      // channels that meet in LDS at a time
-    __shared__ float meet[kWaves][16][LD];
-    __shared__ float2 meet_ml[kWaves][16];
+    constexpr int NS = 2, STAGE = 32 * D + 128, PIECES = D / 64, LOADS = 2 * PIECES + 1;      // K, V, steps of a tile
+    constexpr int MEET = kWaves * 16 * (LD * 4 + 8), RING = kWaves * NS * STAGE;
+    __shared__ uint4 shared_u4[(RING > MEET ? RING : MEET) / 16];
+    float(*meet)[16][LD] = reinterpret_cast<float(*)[16][LD]>(shared_u4);
+    float2(*meet_ml)[16] = reinterpret_cast<float2(*)[16]>(reinterpret_cast<char *>(shared_u4) + kWaves * 16 * LD * 4);
 
     const int lane = threadIdx.x & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
     const int l16 = lane & 15, q = lane >> 4;
@@ -94,88 +116,8 @@ __global__ __launch_bounds__(kWaves *kWave, D == 256 ? 2 : R == 1 ? 4 : 2) void 
     id /= a.splits;
     const int h = id % c.Hk, b = id / c.Hk;
 
-    int64_t first;
-    const int n = rows_of(c, a, b, first);
-    const int rows = min(n, a.max_rows) * a.group, row0 = row_block * 16 * R;
-    if (row0 >= rows) return;
-    const int page = 1 << c.page_shift;
-    const uint32_t cap = (uint32_t)c.per_sequence << c.page_shift;
-    const uint32_t past = min((uint32_t)max(c.cached[b], 0), cap);
-    // keys that the rows of this workgroup see at all, and that all of them see
-    const int last_row = min(n, (row0 + 16 * R - 1) / a.group + 1);
-    const uint32_t limit = min(past + (uint32_t)(a.mask ? min(n, 64) : last_row), cap);
-    const uint32_t all_see = a.mask ? past : min(past + (uint32_t)(row0 / a.group) + 1, limit);
-
-    // query rows: channels (D / 4) q .. of this lane's row, in the order the nibbles come in
-    v8h qf[R][KD];
-    float bias[R];
-    int row_of[R];
-    uint64_t word[R];
-#pragma unroll
-    for (int r = 0; r < R; ++r) {
-        const int row = row0 + 16 * r + l16, i = row / a.group, hq = h * a.group + row - i * a.group;
-        const bool there = row < rows;
-        row_of[r] = i;
-        word[r] = there && a.mask ? a.mask[first + i] : 0;
-        const __half *src = a.Q + (there ? (first + i) * a.ldq + hq * D : first * a.ldq) + q * (D / 4);
-        float sum = 0.f;
-#pragma unroll
-        for (int d = 0; d < KD; ++d) {
-            const v8h x = *reinterpret_cast<const v8h *>(src + 8 * d);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) sum += (float)x[e];
-            qf[r][d] = v8h{x[0], x[4], x[1], x[5], x[2], x[6], x[3], x[7]};
-        }
-        bias[r] = -8.f * 0x1p-18f * quarter_sum(sum);
-    }
-
-    const int half_codes = page * (D / 2);
-    const uint32_t k_lane = l16 * (D / 2) + q * (D / 8), v_lane = half_codes + lane * (D / 8);
-    const int64_t head_at = (int64_t)h * (2 * half_codes), steps_at = cache_steps_at(c.Hk, D, page) + (int64_t)h * page * 2;
-    const int64_t v_steps = (int64_t)c.Hk * page * 2;
-    const int32_t *table = c.table + (int64_t)b * c.per_sequence;
-    // page numbers of the two halves of a tile (their keys clamped to the last there is)
-    auto pages_of = [&](uint32_t tile, int(&number)[2]) {
-#pragma unroll
-        for (int f = 0; f < 2; ++f) number[f] = table[min(tile * kKeysPerTile + 16 * f, limit - 1) >> c.page_shift];
-    };
-    // a page that does not exist is read as page 0, and masked
-    auto page_ok = [&](int number) { return number >= 0 && number < c.pages; };
-    auto page_at = [&](int number) { return c.base + (int64_t)(page_ok(number) ? number : 0) * c.page_bytes; };
-    // slots of a half behind the last key lie in the same page, written or not
-    auto slot_of = [&](uint32_t tile, int f) { return (int)((tile * kKeysPerTile + 16 * f) & (uint32_t)(page - 1)); };
-
-    typedef uint32_t dwords __attribute__((ext_vector_type(KD)));
-    dwords kx[2], vx[2];
-    v4hs ks[2], vs[2];
-    auto load_codes = [&](dwords(&x)[2], uint32_t tile, const int(&number)[2], uint32_t lane_at) {
-#pragma unroll
-        for (int f = 0; f < 2; ++f)
-            x[f] = *reinterpret_cast<const dwords *>(page_at(number[f]) + head_at + slot_of(tile, f) * (D / 2) + lane_at);
-    };
-    auto load_steps = [&](uint32_t tile, const int(&number)[2]) {
-#pragma unroll
-        for (int f = 0; f < 2; ++f) {
-            const uint8_t *at = page_at(number[f]) + steps_at + 2 * slot_of(tile, f) + 8 * q;
-            ks[f] = *reinterpret_cast<const v4hs *>(at);
-            vs[f] = *reinterpret_cast<const v4hs *>(at + v_steps);
-        }
-    };
-
-    v4f o[R][VT], weights[R];
-    float M[R], l[R];
-#pragma unroll
-    for (int r = 0; r < R; ++r) {
-        M[r] = kNothing;
-        l[r] = 0.f;
-        weights[r] = v4f{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int j = 0; j < VT; ++j) o[r][j] = v4f{0.f, 0.f, 0.f, 0.f};
-    }
-    const v8h ones = {1, 1, 1, 1, 1, 1, 1, 1};
-
     uint32_t chunk_end = (uint32_t)(split + 1) * a.tiles_per_chunk;
-    const uint32_t to_next_chunk = (uint32_t)(a.splits - 1) * a.tiles_per_chunk, tiles = (limit + kKeysPerTile - 1) / kKeysPerTile;
+    const uint32_t to_next_chunk = (uint32_t)(a.splits - 1) * a.tiles_per_chunk;
     auto following = [&](uint32_t tile) {
         tile += kWaves;
         if (tile >= chunk_end) {
@@ -184,142 +126,219 @@ __global__ __launch_bounds__(kWaves *kWave, D == 256 ? 2 : R == 1 ? 4 : 2) void 
         }
         return tile;
     };
-    uint32_t tile = (uint32_t)split * a.tiles_per_chunk + wave;
-    if (tile < tiles) {
-        int number[2], number_n[2];
+    // (constant address space: scalar loads, also between the requests, whose assembly may write any other memory)
+    typedef const __attribute__((address_space(4))) int32_t *Table;
+    const Table table = (Table)(uintptr_t)(c.table + (int64_t)b * c.per_sequence);
+    // Page numbers of the two halves of a tile, by the table alone (the first ones are on their way before the sequence's
+    // length is known).  Slots behind the last key lie in some page, written or not; a page that does not exist is read as
+    // page 0: both are masked.
+    constexpr int NP = ONE_PAGE ? 1 : 2;
+    auto pages_of = [&](uint32_t tile, int(&number)[NP]) {
+#pragma unroll
+        for (int f = 0; f < NP; ++f) number[f] = table[min((tile * kKeysPerTile + 16 * f) >> c.page_shift, (uint32_t)c.per_sequence - 1)];
+    };
+    // The tile at work and the two behind it.  Their pages and the sequence's numbers are one latency: the table has a row
+    // for every sequence.
+    uint32_t tile = (uint32_t)split * a.tiles_per_chunk + wave, tile_1 = following(tile), tile_2 = following(tile_1), stage = 0;
+    int number[NP] = {}, number_1[NP] = {}, number_2[NP] = {};
+    if (c.per_sequence > 0) {
         pages_of(tile, number);
-        uint32_t tile_n = following(tile);
-        pages_of(min(tile_n, tiles - 1), number_n);
-        load_codes(kx, tile, number, k_lane);
-        load_steps(tile, number);
-        load_codes(vx, tile, number, v_lane);
-        while (true) {
-            const bool more = tile_n < tiles;
-            const uint32_t tile_l = more ? tile_n : tile;              // behind the last tile: that one again, unused
-            const int number_l[2] = {more ? number_n[0] : number[0], more ? number_n[1] : number[1]};
-            // scores
-            v4f s[R][2];
-#pragma unroll
-            for (int r = 0; r < R; ++r)
-#pragma unroll
-                for (int f = 0; f < 2; ++f) s[r][f] = v4f{bias[r], bias[r], bias[r], bias[r]};
-#pragma unroll
-            for (int d = 0; d < KD; ++d)
-#pragma unroll
-                for (int f = 0; f < 2; ++f) {
-                    const uint32_t x = kx[f][d];
-                    const v4i w = {(int)((x << 6) & 0x03C003C0u), (int)((x << 2) & 0x03C003C0u), (int)((x >> 2) & 0x03C003C0u),
-                                   (int)((x >> 6) & 0x03C003C0u)};
-#pragma unroll
-                    for (int r = 0; r < R; ++r)
-                        s[r][f] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(v8h, w), qf[r][d], s[r][f], 0, 0, 0);
-                }
-            load_codes(kx, tile_l, number_l, k_lane);
-            const uint32_t tile_2 = following(tile_l);
-            int number_2[2];
-            pages_of(min(tile_2, tiles - 1), number_2);
-
-            // scores times steps; keys that a row does not see
-            const uint32_t key0 = tile * kKeysPerTile;
-            const bool cut = key0 + kKeysPerTile > all_see || !page_ok(number[0]) || !page_ok(number[1]);
-            float step_v[2][4];
-#pragma unroll
-            for (int f = 0; f < 2; ++f)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    step_v[f][e] = (float)vs[f][e];
-#pragma unroll
-                    for (int r = 0; r < R; ++r) s[r][f][e] *= (float)ks[f][e] * a.score_scale;
-                }
-            float step_exponent[2][4];                   // 2^ of it is over the value's step
-#pragma unroll
-            for (int f = 0; f < 2; ++f)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) step_exponent[f][e] = (float)__builtin_amdgcn_frexp_expf(step_v[f][e]);
-            if (cut) {
-#pragma unroll
-                for (int f = 0; f < 2; ++f)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const uint32_t key = key0 + 16 * f + 4 * q + e;
-                        const bool in = key < limit && page_ok(number[f]);
-                        const int new_row = (int)(key - past);
-                        if (!in) step_v[f][e] = step_exponent[f][e] = 0.f;
-#pragma unroll
-                        for (int r = 0; r < R; ++r) {
-                            const bool sees = in && (key < past || (a.mask ? ((word[r] >> (new_row & 63)) & 1) != 0 : new_row <= row_of[r]));
-                            s[r][f][e] = sees ? s[r][f][e] : -INFINITY;
-                        }
-                    }
-            }
-            load_steps(tile_l, number_l);
-            v8h p[R];
-#pragma unroll
-            for (int r = 0; r < R; ++r) {
-                float want = -INFINITY;
-#pragma unroll
-                for (int e = 0; e < 8; ++e) want = fmaxf(want, s[r][e / 4][e % 4] + step_exponent[e / 4][e % 4]);
-                want = quarter_max(want);
-                if (__any(want > M[r] + 6.f)) {
-                    const float M_new = fmaxf(M[r], want), fade = __builtin_amdgcn_exp2f(M[r] - M_new);
-                    M[r] = M_new;
-                    l[r] *= fade;
-                    weights[r] *= fade;
-#pragma unroll
-                    for (int j = 0; j < VT; ++j) o[r][j] *= fade;
-                }
-                float w[8];
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    w[e] = __builtin_amdgcn_exp2f(s[r][e / 4][e % 4] - M[r]);
-                    p[r][e] = (_Float16)(w[e] * step_v[e / 4][e % 4]);
-                }
-                l[r] += ((w[0] + w[1]) + (w[2] + w[3])) + ((w[4] + w[5]) + (w[6] + w[7]));
-                weights[r] = __builtin_amdgcn_mfma_f32_16x16x32_f16(ones, p[r], weights[r], 0, 0, 0);
-            }
-            // values: unit lane % 16 of eight keys, two keys of one channel to a dword
-            auto unit_byte = [&](int f, int key, int i, uint32_t &from, int &byte) {
-                const int at = key * (D / 32) + i;
-                from = vx[f][at / 4];
-                byte = at % 4;
-            };
-#pragma unroll
-            for (int i = 0; i < D / 32; ++i) {
-                v4i even, odd;
-#pragma unroll
-                for (int d = 0; d < 4; ++d) {
-                    uint32_t x0, x1;
-                    int b0, b1;
-                    unit_byte(d / 2, 2 * (d % 2), i, x0, b0);
-                    unit_byte(d / 2, 2 * (d % 2) + 1, i, x1, b1);
-                    const uint32_t t = __builtin_amdgcn_perm(x1, x0, 0x0C000C00u | (uint32_t)b0 | ((uint32_t)(4 + b1) << 16));
-                    even[d] = (int)((t << 6) & 0x03C003C0u);
-                    odd[d] = (int)((t << 2) & 0x03C003C0u);
-                }
-#pragma unroll
-                for (int r = 0; r < R; ++r) {
-                    o[r][2 * i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(v8h, even), p[r], o[r][2 * i], 0, 0, 0);
-                    o[r][2 * i + 1] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(v8h, odd), p[r], o[r][2 * i + 1], 0, 0, 0);
-                }
-            }
-            if (!more) break;
-            load_codes(vx, tile_l, number_l, v_lane);
-            tile = tile_n;
-            tile_n = tile_2;
-#pragma unroll
-            for (int f = 0; f < 2; ++f) {
-                number[f] = number_n[f];
-                number_n[f] = number_2[f];
-            }
-        }
+        pages_of(tile_1, number_1);
+        pages_of(tile_2, number_2);
     }
 
-    // the waves' sums meet, 16 rows and CB channels at a time
+    int64_t first;
+    const int n = rows_of(c, a, b, first);
+    const int rows = min(n, a.max_rows) * a.group, row0 = row_block * 16;
+    if (row0 >= rows) return;
+    const int page = 1 << c.page_shift;
+    const uint32_t cap = (uint32_t)c.per_sequence << c.page_shift;
+    const uint32_t past = min((uint32_t)max(c.cached[b], 0), cap);
+    // keys that the rows of this workgroup see at all, and that all of them see
+    const int last_row = min(n, (row0 + 16 - 1) / a.group + 1);
+    const uint32_t limit = min(past + (uint32_t)(a.mask ? min(n, 64) : last_row), cap);
+    const uint32_t all_see = a.mask ? past : min(past + (uint32_t)(row0 / a.group) + 1, limit);
+
+    const uint32_t half_codes = (uint32_t)page * (D / 2), head_at = (uint32_t)h * 2 * half_codes;
+    const uint32_t steps_at = (uint32_t)cache_steps_at(c.Hk, D, page) + (uint32_t)(h * page) * 2, v_steps = (uint32_t)(c.Hk * page) * 2;
+    auto page_ok = [&](int number) { return number >= 0 && number < c.pages; };
+    // A tile in LDS: K's 32 rows, V's two blocks, the steps of K and of V.
+    char *ring = reinterpret_cast<char *>(shared_u4) + wave * (NS * STAGE);
+    const uint32_t ring_at = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)ring;
+    auto request = [&](uint32_t tile, uint32_t stage, const int(&number)[NP]) {
+        const uint8_t *codes[2], *steps[2];
 #pragma unroll
-    for (int r = 0; r < R; ++r) {
-        if (row0 + 16 * r >= rows) break;
-        const float sum = quarter_sum(l[r]);
-        if (q == 0) meet_ml[wave][l16] = float2{M[r], sum};
+        for (int f = 0; f < 2; ++f) {
+            const int no = number[f % NP];
+            const uint8_t *at = c.base + (int64_t)(page_ok(no) ? no : 0) * c.page_bytes;
+            const uint32_t slot = (tile * kKeysPerTile + 16 * f) & (uint32_t)(page - 1);
+            codes[f] = at + (head_at + slot * (D / 2));
+            steps[f] = at + (steps_at + 2 * slot);
+        }
+        const uint32_t to = ring_at + stage * STAGE;
+#pragma unroll
+        for (int u = 0; u < 2 * PIECES; ++u) {
+            const int piece = u % PIECES;                                      // 1024 bytes, in half `half` or (D = 64) in both
+            const uint32_t in = u < PIECES ? 0 : half_codes;
+            if constexpr (ONE_PAGE) {
+                dma_16(codes[0], in + 1024 * piece + 16 * lane, to + 1024 * u);
+            } else if constexpr (D == 64) {
+                dma_16((lane < 32 ? codes[0] : codes[1]) + (in + 16 * (lane & 31)), to + 1024 * u);
+            } else {
+                constexpr int per_half = PIECES / 2;
+                dma_16(codes[piece / per_half], in + 1024 * (piece % per_half) + 16 * lane, to + 1024 * u);
+            }
+        }
+        if (lane < 32)
+            dma_4((ONE_PAGE || !(lane & 8) ? steps[0] + 4 * (lane & (ONE_PAGE ? 15 : 7)) : steps[1] + 4 * (lane & 7)) + (lane & 16 ? v_steps : 0),
+                  to + 32 * D);
+    };
+
+    v4f o[VT], weights = {0.f, 0.f, 0.f, 0.f};
+    float M = kNothing, l = 0.f;
+#pragma unroll
+    for (int j = 0; j < VT; ++j) o[j] = v4f{0.f, 0.f, 0.f, 0.f};
+    const v8h ones = {1, 1, 1, 1, 1, 1, 1, 1};
+
+    const uint32_t tiles = (limit + kKeysPerTile - 1) / kKeysPerTile;
+    bool ok[NP], ok_1[NP];             // whether the pages of the first two exist
+    auto exist = [&](bool(&ok)[NP], const int(&number)[NP]) {
+#pragma unroll
+        for (int f = 0; f < NP; ++f) ok[f] = page_ok(number[f]);
+    };
+    exist(ok, number);
+    exist(ok_1, number_1);
+    if (tile < tiles) request(tile, 0, number);
+    if (tile_1 < tiles) request(tile_1, 1, number_1);
+
+    // query rows: channels (D / 4) q .. of this lane's row, in the order the nibbles come in
+    v8h qf[KD];
+    const int row = row0 + l16, new_row_of = row / a.group;
+    const bool there = row < rows;
+    const uint64_t word = there && a.mask ? a.mask[first + new_row_of] : 0;
+    float bias;
+    {
+        const __half *src = a.Q + (there ? (first + new_row_of) * a.ldq + (h * a.group + row - new_row_of * a.group) * D : first * a.ldq) + q * (D / 4);
+        float sum = 0.f;
+#pragma unroll
+        for (int d = 0; d < KD; ++d) {
+            const v8h x = *reinterpret_cast<const v8h *>(src + 8 * d);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) sum += (float)x[e];
+            qf[d] = v8h{x[0], x[4], x[1], x[5], x[2], x[6], x[3], x[7]};
+        }
+        bias = -8.f * 0x1p-20f * quarter_sum(sum);
+    }
+
+    while (tile < tiles) {
+        // this tile has landed once only the requests behind it are outstanding
+        if (tile_1 < tiles)
+            wait_vmcnt<LOADS>();
+        else
+            wait_vmcnt<0>();
+        const char *in = ring + stage * STAGE;
+        typedef uint32_t dwords __attribute__((ext_vector_type(KD)));
+        dwords kx[2], vx[2];
+        v4hs ks[2], vs[2];
+#pragma unroll
+        for (int f = 0; f < 2; ++f) {
+            kx[f] = *reinterpret_cast<const dwords *>(in + f * (8 * D) + l16 * (D / 2) + q * (D / 8));
+            ks[f] = *reinterpret_cast<const v4hs *>(in + 32 * D + 32 * f + 8 * q);
+            vs[f] = *reinterpret_cast<const v4hs *>(in + 32 * D + 64 + 32 * f + 8 * q);
+            vx[f] = *reinterpret_cast<const dwords *>(in + (16 + 8 * f) * D + lane * (D / 8));
+        }
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");             // the stage has been read: it may be requested again
+        bool ok_2[NP];
+        exist(ok_2, number_2);
+        if (tile_2 < tiles) request(tile_2, stage, number_2);
+        const uint32_t tile_3 = following(tile_2);
+        pages_of(tile_3, number_2);
+
+        v4f s[2];
+#pragma unroll
+        for (int f = 0; f < 2; ++f) s[f] = v4f{bias, bias, bias, bias};
+#pragma unroll
+        for (int d = 0; d < KD; ++d)
+#pragma unroll
+            for (int f = 0; f < 2; ++f) {
+                const uint32_t x = kx[f][d];
+                const v4i w = {(int)((x << 4) & 0x00F000F0u), (int)(x & 0x00F000F0u), (int)((x >> 4) & 0x00F000F0u), (int)((x >> 8) & 0x00F000F0u)};
+                s[f] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(v8h, w), qf[d], s[f], 0, 0, 0);
+            }
+        // scores times steps (the mixed-precision multiply-add takes the fp16 as it is); keys that a row does not see
+        float step_v[8], step_log[8];                  // fp32 bits as a number: 2^23 (127 + log2), to within 0.09 2^23 below
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            step_v[e] = (float)vs[e / 4][e % 4];
+            step_log[e] = (float)__builtin_bit_cast(int, step_v[e]);
+            s[e / 4][e % 4] = __builtin_fmaf(s[e / 4][e % 4], (float)ks[e / 4][e % 4], 0.f);
+        }
+        const uint32_t key0 = tile * kKeysPerTile;
+        if (key0 + kKeysPerTile > all_see || !ok[0] || !ok[NP - 1]) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const uint32_t key = key0 + 16 * (e / 4) + 4 * q + e % 4;
+                const int new_key = (int)(key - past);
+                const bool written = (key < limit) & ok[e / 4 % NP], by_mask = (word >> (new_key & 63)) & 1, by_order = new_key <= new_row_of;
+                const bool sees = written & ((key < past) | (a.mask ? by_mask : by_order));        // no branches
+                if (!written) step_v[e] = step_log[e] = 0.f;
+                s[e / 4][e % 4] = sees ? s[e / 4][e % 4] : -INFINITY;
+            }
+        }
+        float want[8], w[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) want[e] = __builtin_fmaf(s[e / 4][e % 4], a.score_scale * 0x1p23f, step_log[e]);
+        const float most = __builtin_fmaf(quarter_max(fmaxf(fmaxf(fmaxf(want[0], want[1]), fmaxf(want[2], want[3])),
+                                                            fmaxf(fmaxf(want[4], want[5]), fmaxf(want[6], want[7])))), 0x1p-23f, -127.f);
+        if (__any(most > M + 6.f)) {
+            // up by what the roundings of `most` and of the exponents below may be off, which counts where scores are huge only
+            const float up = fmaxf(most, kNothing), M_new = fmaxf(M, __builtin_fmaf(fabsf(up), 0x1p-22f, up)), fade = __builtin_amdgcn_exp2f(M - M_new);
+            M = M_new;
+            l *= fade;
+            weights *= fade;
+#pragma unroll
+            for (int j = 0; j < VT; ++j) o[j] *= fade;
+        }
+        v8h p;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            w[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e / 4][e % 4], a.score_scale, -M));
+            p[e] = (_Float16)(w[e] * step_v[e]);
+        }
+        l += ((w[0] + w[1]) + (w[2] + w[3])) + ((w[4] + w[5]) + (w[6] + w[7]));
+        weights = __builtin_amdgcn_mfma_f32_16x16x32_f16(ones, p, weights, 0, 0, 0);
+        // values: unit lane % 16 of eight keys, two keys of one channel to a dword
+#pragma unroll
+        for (int i = 0; i < D / 32; ++i) {
+            v4i even, odd;
+#pragma unroll
+            for (int d = 0; d < 4; ++d) {
+                // byte i of the units of keys 2 (d % 2) and the next one
+                const int at0 = 2 * (d % 2) * (D / 32) + i, at1 = at0 + D / 32;
+                const uint32_t t = __builtin_amdgcn_perm(vx[d / 2][at1 / 4], vx[d / 2][at0 / 4],
+                                                         0x0C000C00u | (uint32_t)(at0 % 4) | ((uint32_t)(4 + at1 % 4) << 16));
+                even[d] = (int)((t << 4) & 0x00F000F0u);
+                odd[d] = (int)(t & 0x00F000F0u);
+            }
+            o[2 * i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(v8h, even), p, o[2 * i], 0, 0, 0);
+            o[2 * i + 1] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(v8h, odd), p, o[2 * i + 1], 0, 0, 0);
+        }
+        tile = tile_1;
+        tile_1 = tile_2;
+        tile_2 = tile_3;
+#pragma unroll
+        for (int f = 0; f < NP; ++f) {
+            ok[f] = ok_1[f];
+            ok_1[f] = ok_2[f];
+        }
+        stage ^= 1;
+    }
+    __syncthreads();                                   // the ring becomes the place where the sums meet
+
+    // the waves' sums meet, CB channels at a time
+    {
+        const float sum = quarter_sum(l);
+        if (q == 0) meet_ml[wave][l16] = float2{M, sum};
 #pragma unroll
         for (int cb = 0; cb < D / CB; ++cb) {
             if (q * (D / 4) / CB == cb) {
@@ -327,15 +346,15 @@ __global__ __launch_bounds__(kWaves *kWave, D == 256 ? 2 : R == 1 ? 4 : 2) void 
                 for (int e = 0; e < 4; ++e)
 #pragma unroll
                     for (int j = 0; j < VT; j += 4) {
-                        const float off = -8.f * weights[r][e];
+                        const float off = -8.f * weights[e];
                         *reinterpret_cast<float4 *>(&meet[wave][l16][q * (D / 4) % CB + e * VT + j]) =
-                            float4{__builtin_fmaf(o[r][j][e], 0x1p18f, off), __builtin_fmaf(o[r][j + 1][e], 0x1p18f, off),
-                                   __builtin_fmaf(o[r][j + 2][e], 0x1p18f, off), __builtin_fmaf(o[r][j + 3][e], 0x1p18f, off)};
+                            float4{__builtin_fmaf(o[j][e], 0x1p20f, off), __builtin_fmaf(o[j + 1][e], 0x1p20f, off),
+                                   __builtin_fmaf(o[j + 2][e], 0x1p20f, off), __builtin_fmaf(o[j + 3][e], 0x1p20f, off)};
                     }
             }
             __syncthreads();
             constexpr int PER = CB / 16;                               // channels per thread
-            const int mine = threadIdx.x / 16, at = (threadIdx.x % 16) * PER, row = row0 + 16 * r + mine;
+            const int mine = threadIdx.x / 16, at = (threadIdx.x % 16) * PER, row = row0 + mine;
             if (row < rows) {
                 float top = kNothing, total = 0.f, out[PER] = {};
 #pragma unroll
@@ -427,12 +446,12 @@ __global__ __launch_bounds__(256) void tree_attention_join_kernel(const CacheVie
     *reinterpret_cast<v4hs *>(a.O + (first + i) * a.ldo + hq * D + 4 * mine) = y;
 }
 
-template <int D, int R>
+template <int D, bool ONE_PAGE>
 sq_status launch_tree_attention(const CacheView &c, const AttentionCall &a, hipStream_t st)
 {
     const int64_t blocks = (int64_t)a.row_blocks * a.splits * c.Hk * c.B;
     if (blocks > 0x7FFFFFFF) return SQ_ERR_SHAPE;
-    hipLaunchKernelGGL((tree_attention_kernel<D, R>), dim3((unsigned)blocks), dim3(kWaves * kWave), 0, st, c, a);
+    hipLaunchKernelGGL((tree_attention_kernel<D, ONE_PAGE>), dim3((unsigned)blocks), dim3(kWaves * kWave), 0, st, c, a);
     if (hipGetLastError() != hipSuccess) return SQ_ERR_LAUNCH;
     if (a.splits == 1) return SQ_OK;
     const int64_t units = (int64_t)a.max_rows * a.Hq;
@@ -446,13 +465,14 @@ sq_status dispatch_tree_attention(const CacheView &c, AttentionCall &a, int64_t 
                                   hipStream_t st)
 {
     const int64_t rows = (int64_t)a.max_rows * a.group;
-    const int tiles = rows <= 16 ? 1 : 2;
     if (rows > (1 << 30)) return SQ_ERR_SHAPE;
-    a.row_blocks = (int)((rows + 16 * tiles - 1) / (16 * tiles));
-    // as many splits as give every CU four workgroups, chunks of at least 128 keys, and what the workspace holds
+    a.row_blocks = (int)((rows + 15) / 16);
+    // As many splits as keep the workgroups within the four that a CU holds (a few more would make a second round), chunks of
+    // at least 128 keys, and what the workspace holds.  (us at 48 sequences of 8192 keys, 8 heads: two splits, 768 workgroups,
+    // 95; three, 1152 of them, 111; 16 trees, 1536 workgroups without a split 107, with two 151.)
     const int64_t units = (int64_t)a.row_blocks * c.Hk * c.B;
     max_keys = max_keys < 1 ? 1 : max_keys;
-    int64_t splits = (1024 + units - 1) / units;
+    int64_t splits = 1024 / units;
     const int64_t chunks = (max_keys + kChunkUnit - 1) / kChunkUnit, room = workspace_bytes / (a.T * a.Hq * (D + 2) * 4);
     splits = splits < chunks ? splits : chunks;
     splits = splits < kMaxSplits ? splits : kMaxSplits;
@@ -460,7 +480,7 @@ sq_status dispatch_tree_attention(const CacheView &c, AttentionCall &a, int64_t 
     a.splits = splits < 1 ? 1 : (int)splits;
     a.part = static_cast<float *>(workspace);
     a.tiles_per_chunk = kWaves * (int)((chunks + a.splits - 1) / a.splits);
-    return tiles == 1 ? launch_tree_attention<D, 1>(c, a, st) : launch_tree_attention<D, 2>(c, a, st);
+    return c.page_shift > 4 ? launch_tree_attention<D, true>(c, a, st) : launch_tree_attention<D, false>(c, a, st);
 }
 
 }  // namespace
@@ -482,7 +502,7 @@ extern "C" sq_status sq_tree_attention(const void *Q, int64_t ldq, int64_t T, in
     const sq_status s = sq::check_cache(Hk, D, page, B, per_sequence, pages);
     if (s != SQ_OK) return s;
     if (T < 0 || T > SQ_MAX_ROWS || Hq <= 0 || Hq > 65536 || (Hq % Hk) != 0) return SQ_ERR_SHAPE;
-    if (ldq < (int64_t)Hq * D || ldo < (int64_t)Hq * D || !(scale > 0.f) || !(scale < 1e30f)) return SQ_ERR_SHAPE;
+    if (ldq < (int64_t)Hq * D || ldo < (int64_t)Hq * D || !(scale > 0.f) || !(scale < 1e20f)) return SQ_ERR_SHAPE;
     if (max_rows < 0 || max_keys < 0 || (mask && max_rows > 64) || workspace_bytes < 0) return SQ_ERR_SHAPE;
     if (T == 0 || B == 0 || max_rows == 0) return SQ_OK;
     if (!Q || !O || !row_start || !cached || (!table && per_sequence > 0) || (!cache && pages > 0) || (!workspace && workspace_bytes > 0))
@@ -502,7 +522,7 @@ extern "C" sq_status sq_tree_attention(const void *Q, int64_t ldq, int64_t T, in
     a.Hq = Hq;
     a.group = Hq / Hk;
     a.max_rows = (int)(max_rows < T ? max_rows : T);
-    a.score_scale = (float)((double)scale * 1.4426950408889634 * 262144.0);
+    a.score_scale = (float)((double)scale * 1.4426950408889634 * 1048576.0);
     const hipStream_t st = static_cast<hipStream_t>(stream);
     if (D == 64) return sq::dispatch_tree_attention<64>(c, a, max_keys, workspace, workspace_bytes, st);
     if (D == 128) return sq::dispatch_tree_attention<128>(c, a, max_keys, workspace, workspace_bytes, st);

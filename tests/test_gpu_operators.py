@@ -408,6 +408,31 @@ def test_attention_scores_far_apart():
     ou.held(s.run(Q, None, 1000.0), want, bound, "tiny queries")
 
 
+def test_attention_largest_scores():
+    """Scores of millions: one key takes it all, nothing overflows; beyond what fp32 tells apart the result is still finite."""
+    print("case attention largest scores", flush=True)
+    s = Setting(78, [500, 40], [2, 1], 2, 64, 16)
+    Q = (s.queries(4) * np.float16(3000)).astype(np.float16)
+    got = s.run(Q, None, 5.0)
+    assert np.isfinite(got.astype(np.float64)).all()
+    for b in range(2):
+        k = s.numbers.values(b, 0, int(s.past[b] + s.new[b]))[0]
+        v, sv = s.numbers.values(b, 1, int(s.past[b] + s.new[b]))
+        for t in range(s.start[b], s.start[b + 1]):
+            L = int(s.past[b] + t - s.start[b] + 1)
+            for h in range(4):
+                order = np.argsort(k[:L, h // 2] @ Q[t, h].astype(np.float64))
+                top2 = (k[order[-2:], h // 2] @ Q[t, h].astype(np.float64)) * 5.0
+                if top2[1] - top2[0] > 64:                  # the rest is below 2^-90
+                    # the weight and the result are rounded to fp16 (half a step each, the second one of the first's
+                    # result); the eights come off sums of 16 steps a term, as in operators_util.attention
+                    x = v[order[-1], h // 2]
+                    bound = (2 * ou.HALF + ou.HALF ** 2 + 8 * ou.EPS32) * np.abs(x) + 40 * ou.EPS32 * 16 * sv[order[-1], h // 2] + ou.TINY
+                    ou.held(got[t, h], x, bound, f"{b} {t} {h}")
+    Q[:] = 60000.0
+    assert np.isfinite(s.run(Q, None, 1e6).astype(np.float64)).all()
+
+
 def test_attention_pages_that_do_not_exist():
     print("case attention bad pages", flush=True)
     s = Setting(300, [100, 40], [2, 2], 2, 128, 16)
