@@ -17,6 +17,7 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 _LIB_PATH = os.path.join(_HERE, "libsinglequant.so")
 _lib = None
 _torch = None
+_f16 = _u8 = _i32 = _i64 = _raw_stream = _raw_device = None       # torch's, once it is loaded
 _I32, _F32 = np.dtype(np.int32), np.dtype(np.float32)
 
 SQ_OK = 0
@@ -33,7 +34,7 @@ def library_path() -> str:
 
 
 def _load():
-    global _lib, _torch
+    global _lib, _torch, _f16, _u8, _i32, _i64, _raw_stream, _raw_device
     if _lib is None:
         if not os.path.exists(_LIB_PATH):
             raise RuntimeError(
@@ -45,6 +46,8 @@ def _load():
         # runtimes, and the one the library talks to reports "no ROCm-capable device".
         import torch
         _torch = torch
+        _f16, _u8, _i32, _i64 = torch.float16, torch.uint8, torch.int32, torch.int64
+        _raw_stream, _raw_device = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice
         lib = C.CDLL(_LIB_PATH)
         lib.sq_rotate_quantize.restype = C.c_int
         lib.sq_rotate_quantize.argtypes = [
@@ -456,64 +459,71 @@ def sq_prepare_weights_variant(W, giv_i, giv_j, giv_theta, R1, R2, bits, clip_ra
     _check(code)
 
 
-def _is(t, dtype, name, contiguous=True):
-    """Integer arrays and steps travel as bare pointers: their type and layout are checked here."""
-    if t.dtype is not dtype:
-        raise ValueError(f"{name} must be {dtype}")
-    if contiguous and not t.is_contiguous():
-        raise ValueError(f"{name} must be contiguous")
+# The calls below check types and layouts of what travels as bare pointers, in few Python steps: at one token a call is
+# bound by the host (3 us of launch, 2 to 4 here).
 
 
-def _heads(t, name, dtype):
-    """[T, H, D] whose heads have contiguous channels: T, H, D, token stride, head stride."""
+def _layout(*wanted):
+    """Says which of (name, tensor, dtype, contiguous) is not as it must be; called once something is not."""
+    for name, t, dtype, contiguous in wanted:
+        if t.dtype is not dtype:
+            raise ValueError(f"{name} must be {dtype}")
+        if contiguous and not t.is_contiguous():
+            raise ValueError(f"{name} must be contiguous")
+    raise ValueError("the channels of a row must be contiguous")
+
+
+def _heads(t, name, packed=True):
+    """fp16 [T, H, D] whose heads have contiguous channels (packed: and lie side by side): shape, token and head stride."""
     T, H, D = t.shape
-    if t.dtype is not dtype:
-        raise ValueError(f"{name} must be {dtype}")
-    if D > 1 and t.stride(2) != 1:
-        raise ValueError(f"{name}: the channels of a head must be contiguous")
-    head = t.stride(1) if H > 1 else D
-    return T, H, D, (t.stride(0) if T > 1 else max(H - 1, 0) * head + D), head
+    row, head, one = t.stride()
+    if H <= 1:
+        head = D
+    if T <= 1:
+        row = max(H - 1, 0) * head + D
+    if t.dtype is not _f16:
+        raise ValueError(f"{name} must be {_f16}")
+    if (one != 1 and D > 1) or (packed and head != D):
+        raise ValueError(f"{name}: the channels of a head must be contiguous" + (", the heads side by side" if packed else ""))
+    return T, H, D, row, head
 
 
-def _packed_heads(t, name):
-    """_heads of fp16 rows whose heads lie side by side; a row's stride is a multiple of 8 in any case."""
-    T, H, D, ld, head = _heads(t, name, _torch.float16)
-    if head != D:
-        raise ValueError(f"{name}: the heads of a row must lie side by side")
-    return T, H, D, ld
+def _here(stream):
+    return _raw_stream(_raw_device()) if stream is None else stream.cuda_stream
 
 
 def sq_quantize_grouped(X, group, Q, steps, stream=None) -> None:
     """X fp16 [T, K] to codes Q uint8 [T, K/2] with steps fp16 [T, K / group]."""
-    lib = _load()
+    lib = _lib or _load()
     T, K = X.shape
-    _is(X, _torch.float16, "X", False)
-    _is(Q, _torch.uint8, "Q")
-    _is(steps, _torch.float16, "steps")
-    if group <= 0 or tuple(Q.shape) != (T, K // 2) or tuple(steps.shape) != (T, K // group):
+    ldx, one = X.stride()
+    if X.dtype is not _f16 or Q.dtype is not _u8 or steps.dtype is not _f16 or not Q.is_contiguous() or not steps.is_contiguous() or (
+            one != 1 and K > 1):
+        _layout(("X", X, _f16, False), ("Q", Q, _u8, True), ("steps", steps, _f16, True))
+    if group <= 0 or Q.shape != (T, K // 2) or steps.shape != (T, K // group):
         raise ValueError("Q must be [T, K/2] and steps [T, K / group]")
-    if K > 1 and X.stride(1) != 1:
-        raise ValueError("the channels of X must be contiguous")
-    _check(lib.sq_quantize_grouped(X.data_ptr(), T, K, X.stride(0) if T > 1 else K, int(group), Q.data_ptr(),
-                                   steps.data_ptr(), _stream_handle(stream)))
+    code = lib.sq_quantize_grouped(X.data_ptr(), T, K, ldx if T > 1 else K, group, Q.data_ptr(), steps.data_ptr(), _here(stream))
+    if code:
+        _check(code)
 
 
 def sq_w4a16_gemm_grouped(X, Qw, steps, Y, stream=None) -> None:
     """X fp16 [T, K] times weight codes Qw uint8 [N, K/2] with steps fp16 [N, K / group] -> Y fp16 [T, N]; the group is
     what the shapes say."""
-    lib = _load()
+    lib = _lib or _load()
     T, K = X.shape
     N, groups = steps.shape
-    _is(X, _torch.float16, "X", False)
-    _is(Y, _torch.float16, "Y", False)
-    _is(Qw, _torch.uint8, "Qw")
-    _is(steps, _torch.float16, "steps")
-    if groups <= 0 or K % groups or tuple(Qw.shape) != (N, K // 2) or tuple(Y.shape) != (T, N):
+    ldx, one = X.stride()
+    ldy, one_y = Y.stride()
+    if X.dtype is not _f16 or Y.dtype is not _f16 or Qw.dtype is not _u8 or steps.dtype is not _f16 or not (
+            Qw.is_contiguous() and steps.is_contiguous()) or (one != 1 and K > 1) or (one_y != 1 and N > 1):
+        _layout(("X", X, _f16, False), ("Y", Y, _f16, False), ("Qw", Qw, _u8, True), ("steps", steps, _f16, True))
+    if groups <= 0 or K % groups or Qw.shape != (N, K // 2) or Y.shape != (T, N):
         raise ValueError("Qw must be [N, K/2], steps [N, K / group] and Y [T, N]")
-    if (K > 1 and X.stride(1) != 1) or (N > 1 and Y.stride(1) != 1):
-        raise ValueError("the rows of X and Y must be contiguous")
-    _check(lib.sq_w4a16_gemm_grouped(X.data_ptr(), T, K, X.stride(0) if T > 1 else K, Qw.data_ptr(), steps.data_ptr(),
-                                     K // groups, N, Y.data_ptr(), Y.stride(0) if T > 1 else max(N, 1), _stream_handle(stream)))
+    code = lib.sq_w4a16_gemm_grouped(X.data_ptr(), T, K, ldx if T > 1 else K, Qw.data_ptr(), steps.data_ptr(), K // groups, N,
+                                     Y.data_ptr(), ldy if T > 1 else N, _here(stream))
+    if code:
+        _check(code)
 
 
 # sq_rotary_scaling of singlequant.h
@@ -537,15 +547,17 @@ def sq_rotary_table(rot, base=10000.0, scaling=SQ_ROTARY_PLAIN, factor=1.0, trai
 def sq_rotary_fp16(X, positions, turns, half, Y, magnitude=1.0, stream=None) -> None:
     """Rotary positions on X fp16 [T, H, D] (any token and head strides) -> Y of the same shape (may be X).  positions
     int32 [T]; turns int64 [rot / 2] on the device, from sq_rotary_table; half: pairs (i, i + rot / 2), else (2i, 2i + 1)."""
-    lib = _load()
-    T, H, D, ldx, ldh = _heads(X, "X", _torch.float16)
-    _, _, _, ldy, ldyh = _heads(Y, "Y", _torch.float16)
-    _is(positions, _torch.int32, "positions")
-    _is(turns, _torch.int64, "turns")
+    lib = _lib or _load()
+    T, H, D, ldx, ldh = _heads(X, "X", False)
+    ldy, ldyh = (ldx, ldh) if Y is X else _heads(Y, "Y", False)[3:]
+    if positions.dtype is not _i32 or turns.dtype is not _i64 or not (positions.is_contiguous() and turns.is_contiguous()):
+        _layout(("positions", positions, _i32, True), ("turns", turns, _i64, True))
     if Y.shape != X.shape or positions.numel() != T:
         raise ValueError("Y must have the shape of X, positions one entry per token")
-    _check(lib.sq_rotary_fp16(X.data_ptr(), T, H, D, ldx, ldh, positions.data_ptr(), turns.data_ptr(), 2 * turns.numel(),
-                              1 if half else 0, float(magnitude), Y.data_ptr(), ldy, ldyh, _stream_handle(stream)))
+    code = lib.sq_rotary_fp16(X.data_ptr(), T, H, D, ldx, ldh, positions.data_ptr(), turns.data_ptr(), 2 * turns.numel(),
+                              1 if half else 0, magnitude, Y.data_ptr(), ldy, ldyh, _here(stream))
+    if code:
+        _check(code)
 
 
 @functools.lru_cache(maxsize=256)
@@ -553,44 +565,49 @@ def sq_cache_page_bytes(Hk: int, D: int, page: int) -> int:
     return int(_load().sq_cache_page_bytes(int(Hk), int(D), int(page)))
 
 
-def _cache_args(T, Hk, D, row_start, cached, table, page, cache):
+def _cache_args(Hk, D, row_start, cached, table, page, cache):
     """B, per_sequence and pages of a cache (any uint8 tensor that is a whole number of pages)."""
-    _is(row_start, _torch.int32, "row_start")
-    _is(cached, _torch.int32, "cached")
-    _is(table, _torch.int32, "table")
-    _is(cache, _torch.uint8, "cache")
     B, per_sequence = table.shape
+    if row_start.dtype is not _i32 or cached.dtype is not _i32 or table.dtype is not _i32 or cache.dtype is not _u8 or not (
+            row_start.is_contiguous() and cached.is_contiguous() and table.is_contiguous() and cache.is_contiguous()):
+        _layout(("row_start", row_start, _i32, True), ("cached", cached, _i32, True), ("table", table, _i32, True),
+                ("cache", cache, _u8, True))
     if row_start.numel() != B + 1 or cached.numel() != B:
         raise ValueError("table must be [B, pages of a sequence], row_start [B + 1] and cached [B]")
     size = sq_cache_page_bytes(Hk, D, page)
-    if size and cache.numel() % size:
+    pages, rest = divmod(cache.numel(), size) if size else (0, 0)
+    if rest:
         raise ValueError("cache is not a whole number of pages of sq_cache_page_bytes")
-    return B, per_sequence, cache.numel() // size if size else 0
+    return B, per_sequence, pages
 
 
 def sq_cache_append(K, V, row_start, cached, table, page, cache, stream=None) -> None:
     """New rows K, V fp16 [T, Hk, D] (any row strides) into the cache: row_start int32 [B + 1], cached int32 [B], table
     int32 [B, pages of a sequence], cache uint8, pages * sq_cache_page_bytes(Hk, D, page) bytes."""
-    lib = _load()
-    T, Hk, D, ldk = _packed_heads(K, "K")
-    _, _, _, ldv = _packed_heads(V, "V")
+    lib = _lib or _load()
+    T, Hk, D, ldk, _ = _heads(K, "K")
+    ldv = _heads(V, "V")[3]
     if V.shape != K.shape:
         raise ValueError("K and V must have the same shape")
-    B, per_sequence, pages = _cache_args(T, Hk, D, row_start, cached, table, page, cache)
-    _check(lib.sq_cache_append(K.data_ptr(), ldk, V.data_ptr(), ldv, T, Hk, D, row_start.data_ptr(), cached.data_ptr(), B,
-                               table.data_ptr(), per_sequence, int(page), cache.data_ptr(), pages, _stream_handle(stream)))
+    B, per_sequence, pages = _cache_args(Hk, D, row_start, cached, table, page, cache)
+    code = lib.sq_cache_append(K.data_ptr(), ldk, V.data_ptr(), ldv, T, Hk, D, row_start.data_ptr(), cached.data_ptr(), B,
+                               table.data_ptr(), per_sequence, page, cache.data_ptr(), pages, _here(stream))
+    if code:
+        _check(code)
 
 
 def sq_cache_read(cache, row_start, cached, table, page, K, V, stream=None) -> None:
     """The rows that sq_cache_append with the same arrays writes, as fp16 into K, V [T, Hk, D]."""
-    lib = _load()
-    T, Hk, D, ldk = _packed_heads(K, "K")
-    _, _, _, ldv = _packed_heads(V, "V")
+    lib = _lib or _load()
+    T, Hk, D, ldk, _ = _heads(K, "K")
+    ldv = _heads(V, "V")[3]
     if V.shape != K.shape:
         raise ValueError("K and V must have the same shape")
-    B, per_sequence, pages = _cache_args(T, Hk, D, row_start, cached, table, page, cache)
-    _check(lib.sq_cache_read(cache.data_ptr(), pages, Hk, D, row_start.data_ptr(), cached.data_ptr(), B, table.data_ptr(),
-                             per_sequence, int(page), K.data_ptr(), ldk, V.data_ptr(), ldv, T, _stream_handle(stream)))
+    B, per_sequence, pages = _cache_args(Hk, D, row_start, cached, table, page, cache)
+    code = lib.sq_cache_read(cache.data_ptr(), pages, Hk, D, row_start.data_ptr(), cached.data_ptr(), B, table.data_ptr(),
+                             per_sequence, page, K.data_ptr(), ldk, V.data_ptr(), ldv, T, _here(stream))
+    if code:
+        _check(code)
 
 
 def sq_tree_attention_workspace_bytes(T: int, Hq: int, D: int) -> int:
@@ -601,22 +618,27 @@ def sq_tree_attention(Q, row_start, cached, mask, table, page, cache, Hk, scale,
                       stream=None) -> None:
     """Attention of the new rows Q fp16 [T, Hq, D] over the cache -> O [T, Hq, D].  mask int64 [T] (bit j: the row sees new
     row j of its sequence) or None (rows 0 .. i); max_rows: at least the new rows of every sequence; max_keys: about the
-    longest sequence (None: what the table holds); workspace: any device tensor, or None (nothing is split)."""
-    lib = _load()
-    T, Hq, D, ldq = _packed_heads(Q, "Q")
-    _, _, _, ldo = _packed_heads(O, "O")
+    longest sequence (None: what the table holds); workspace: any contiguous device tensor, or None (nothing is split)."""
+    lib = _lib or _load()
+    T, Hq, D, ldq, _ = _heads(Q, "Q")
+    ldo = _heads(O, "O")[3]
     if O.shape != Q.shape:
         raise ValueError("O must have the shape of Q")
-    B, per_sequence, pages = _cache_args(T, Hk, D, row_start, cached, table, page, cache)
-    if mask is not None:
-        _is(mask, _torch.int64, "mask")
-        if mask.numel() != T:
-            raise ValueError("mask must have one word per row")
-    _check(lib.sq_tree_attention(
-        Q.data_ptr(), ldq, T, Hq, Hk, D, row_start.data_ptr(), cached.data_ptr(), B,
-        None if mask is None else mask.data_ptr(), int(max_rows), per_sequence * page if max_keys is None else int(max_keys),
-        table.data_ptr(), per_sequence, int(page), cache.data_ptr(), pages, float(scale), O.data_ptr(), ldo,
-        _dev_ptr(workspace), 0 if workspace is None else workspace.numel() * workspace.element_size(), _stream_handle(stream)))
+    B, per_sequence, pages = _cache_args(Hk, D, row_start, cached, table, page, cache)
+    if mask is not None and (mask.dtype is not _i64 or not mask.is_contiguous() or mask.numel() != T):
+        raise ValueError("mask must be int64, one word per row")
+    if workspace is None:
+        ws, ws_bytes = None, 0
+    else:
+        if not workspace.is_contiguous():
+            raise ValueError("workspace must be contiguous")
+        ws, ws_bytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
+    code = lib.sq_tree_attention(
+        Q.data_ptr(), ldq, T, Hq, Hk, D, row_start.data_ptr(), cached.data_ptr(), B, None if mask is None else mask.data_ptr(),
+        max_rows, per_sequence * page if max_keys is None else max_keys, table.data_ptr(), per_sequence, page, cache.data_ptr(),
+        pages, scale, O.data_ptr(), ldo, ws, ws_bytes, _here(stream))
+    if code:
+        _check(code)
 
 
 def sq_kron_factor(n: int):
