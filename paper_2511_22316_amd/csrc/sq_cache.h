@@ -35,24 +35,40 @@ __device__ __forceinline__ int cache_page(const CacheView &c, int b, int index)
     return number >= 0 && number < c.pages ? number : -1;
 }
 
-// Sequence of new row `row` (the same in every lane of the wave): the last b with row_start[b] <= row.  64 probes at a
-// time: one memory latency up to 64 sequences, two up to 4096.  -1 for a row in front of the first or behind the last.
-__device__ __forceinline__ int sequence_of_row(const int32_t *row_start, int B, int64_t row)
+// A new row's sequence, with what the sequence's arrays say of it.
+struct RowOwner {
+    int b;                     // -1: none
+    int first, cached;         // row_start[b], cached[b]
+};
+
+// The sequence of new row `row` (the same in every lane of the wave): the last b with row_start[b] <= row, if the row is in
+// front of row_start[b + 1].  64 probes at a time, and the last ones bring the sequence's own numbers with them: one memory
+// latency up to 64 sequences, two up to 4096.
+__device__ __forceinline__ RowOwner owner_of_row(const CacheView &c, int64_t row)
 {
     const int lane = (int)(threadIdx.x & (kWave - 1));
-    int lo = 0, count = B;                     // the answer, if there is one, is in lo .. lo + count - 1
-    while (count > 0) {
+    const RowOwner none = {-1, 0, 0};
+    int lo = 0, count = c.B;                   // the answer, if there is one, is in lo .. lo + count - 1
+    while (count > kWave) {
         const int step = (count + kWave - 1) / kWave;
         const int at = lo + lane * step;
-        const bool before = at < lo + count && (int64_t)row_start[at] <= row;
-        const int hits = __popcll(__ballot(before));
-        if (hits == 0) return -1;
+        const int hits = __popcll(__ballot(at < lo + count && (int64_t)c.row_start[at] <= row));
+        if (hits == 0) return none;
         const int next = lo + (hits - 1) * step;
         count = min(step, lo + count - next);
         lo = next;
-        if (step == 1) break;
     }
-    return count > 0 && row < (int64_t)row_start[lo + 1] ? lo : -1;
+    int first = 0, end = 0, cached = 0;
+    const bool there = lane < count;
+    if (there) {
+        first = c.row_start[lo + lane];
+        end = c.row_start[lo + lane + 1];
+        cached = c.cached[lo + lane];
+    }
+    const int hits = __popcll(__ballot(there && (int64_t)first <= row));
+    if (hits == 0) return none;
+    const RowOwner r = {lo + hits - 1, __builtin_amdgcn_readlane(first, hits - 1), __builtin_amdgcn_readlane(cached, hits - 1)};
+    return row < (int64_t)__builtin_amdgcn_readlane(end, hits - 1) ? r : none;
 }
 
 // sizes and pointers that every entry point on a cache checks alike
