@@ -69,9 +69,27 @@ __device__ __forceinline__ int rows_of(const CacheView &c, const AttentionCall &
     return (int)max((int64_t)0, n);
 }
 
-// A workgroup takes one head of K and V of one sequence, 16 query rows (row = new row * group + query head in the group)
+// The sequence with the place-th most keys (64 sequences at most; of more every one in its own place), so that the workgroups
+// of the longest start first: 16 trees of 31 to 61 rows and 2048 to 4096 keys 90 -> 84 us.  It costs a memory latency in front
+// of everything, so one row per sequence goes without (64 sequences of 512 to 1024 keys 21.4 us, 24.5 with it).
+__device__ __forceinline__ int by_length(const CacheView &c, const AttentionCall &a, int place)
+{
+    if (c.B == 1 || c.B > kWave) return place;
+    const int lane = (int)(threadIdx.x & (kWave - 1)), b = min(lane, c.B - 1);
+    int64_t first;
+    const int n = rows_of(c, a, b, first);
+    const uint32_t keys = n > 0 ? (uint32_t)max(c.cached[b], 0) + (uint32_t)n : 0u;
+    const uint32_t key = lane < c.B ? min(keys, (1u << 26) - 1) << 6 | (uint32_t)(kWave - 1 - lane) : 0u;     // all different
+    int longer = lane < c.B ? 0 : kWave;
+    for (int i = 0; i < c.B; ++i) longer += (uint32_t)__builtin_amdgcn_readlane((int)key, i) > key ? 1 : 0;
+    return __builtin_ctzll(__ballot(longer == place));
+}
+
+// A workgroup takes one head of K and V of one sequence, 16 R query rows (row = new row * group + query head in the group)
 // and every splits-th chunk of its keys; its four waves take every fourth tile of 32 keys each and work alone until
-// the end.
+// the end.  What it does per key, whatever the rows, is most of the work of 16 of them (widening the codes: 120 of 260
+// instructions), so more than 16 rows are taken 32 at a time (R = 2), at half the waves per SIMD: the trees above 116 -> 94 us,
+// prompts of 256 to 512 rows 189 -> 128.  Neighbouring workgroups belong to an XCD and have a head of many sequences.
 //
 // Scores: S^T = K Q^T on v_mfma_f32_16x16x32_f16, the keys as rows of the result and the query rows as columns, so a lane has
 // one query row (lane % 16) and four keys of each half of the tile (4 (lane / 16) + r); the weights it makes of them are
@@ -87,19 +105,20 @@ __device__ __forceinline__ int rows_of(const CacheView &c, const AttentionCall &
 // with ones in place of V gives the sum of the weights.
 //
 // Softmax with a running offset M per row: a weight is exp2(s - M) times the value's step, rounded to fp16 (the normaliser
-// keeps the weight in fp32).  M goes by the largest of score plus logarithm of the step; the logarithm is the step's fp32 bits
-// taken as a number, at most 0.09 too small.  The first largest product is 2^7.9 to 2^7.99: just below a power of two, where
-// the steps of fp16 are the finest for it and its followers, and 21 octaves above the subnormals, whatever the values'
-// steps are.  M moves when a product could pass 2^14.  (Outputs were 3.1e-4 off their exact values, in the 2-norm, with a
-// first product of 2^0 or 2^7, 2.7e-4 so; 2.1e-4 is the rounding of the output.  Two fp16 per weight give 2.1e-4 and take
-// 139 us instead of 117 for 16 trees of 64 rows.)
+// keeps the weight in fp32).  M stays as long as no product passes 2^14, which is seen when they are there (the maximum of
+// every tile took 7% more); then it goes by the row's largest sum of a score and the logarithm of the step.  That logarithm is
+// the step's fp32 bits taken as a number, at most 0.09 too small, so the largest product then is 2^7.9 to 2^7.99: just below
+// a power of two, where the steps of fp16 are the finest for it and its followers, and 21 octaves above the subnormals,
+// whatever the values' steps are.  (Outputs were 3.1e-4 off their exact values, in the 2-norm, with a first product of 2^0 or
+// 2^7, 2.7e-4 so; 2.1e-4 is the rounding of the output.  Two fp16 per weight give 2.1e-4 and take 139 us instead of 117 with
+// R = 1.)
 //
 // Loads: global memory -> LDS, two stages per wave; a tile goes to registers as soon as it has landed, and its stage is
 // requested again in front of the work on it, so two tiles are in flight all the time.  A wave waits for its own requests
 // only.  The page numbers are requested a tile ahead of that.
 // ONE_PAGE: pages of 32 rows and more, a tile lies in one.
-template <int D, bool ONE_PAGE>
-__global__ __launch_bounds__(kWaves *kWave, D == 256 ? 2 : 4) void tree_attention_kernel(const CacheView c, const AttentionCall a)
+template <int D, bool ONE_PAGE, int R>
+__global__ __launch_bounds__(kWaves *kWave, D == 256 || R == 2 ? 2 : 4) void tree_attention_kernel(const CacheView c, const AttentionCall a)
 {
     constexpr int KD = D / 32;                       // dwords of K (and of V) per lane and 16 keys; steps of the scores
     constexpr int VT = D / 16;                       // 16-channel tiles of the output
@@ -117,7 +136,7 @@ __global__ __launch_bounds__(kWaves *kWave, D == 256 ? 2 : 4) void tree_attentio
     id /= a.row_blocks;
     const int split = id % a.splits;
     id /= a.splits;
-    const int h = id % c.Hk, b = id / c.Hk;
+    const int h = id / c.B, b = R == 1 ? id % c.B : by_length(c, a, id % c.B);
 
     uint32_t chunk_end = (uint32_t)(split + 1) * a.tiles_per_chunk;
     const uint32_t to_next_chunk = (uint32_t)(a.splits - 1) * a.tiles_per_chunk;
@@ -152,13 +171,13 @@ __global__ __launch_bounds__(kWaves *kWave, D == 256 ? 2 : 4) void tree_attentio
 
     int64_t first;
     const int n = rows_of(c, a, b, first);
-    const int rows = min(n, a.max_rows) * a.group, row0 = row_block * 16;
+    const int rows = min(n, a.max_rows) * a.group, row0 = row_block * (16 * R);
     if (row0 >= rows) return;
     const int page = 1 << c.page_shift;
     const uint32_t cap = (uint32_t)c.per_sequence << c.page_shift;
     const uint32_t past = min((uint32_t)max(c.cached[b], 0), cap);
     // keys that the rows of this workgroup see at all, and that all of them see
-    const int last_row = min(n, (row0 + 16 - 1) / a.group + 1);
+    const int last_row = min(n, (row0 + 16 * R - 1) / a.group + 1);
     const uint32_t limit = min(past + (uint32_t)(a.mask ? min(n, 64) : last_row), cap);
     const uint32_t all_see = a.mask ? past : min(past + (uint32_t)(row0 / a.group) + 1, limit);
 
@@ -197,10 +216,15 @@ __global__ __launch_bounds__(kWaves *kWave, D == 256 ? 2 : 4) void tree_attentio
                   to + 32 * D);
     };
 
-    v4f o[VT], weights = {0.f, 0.f, 0.f, 0.f};
-    float M = kNothing, l = 0.f;
+    v4f o[R][VT], weights[R];
+    float M[R], l[R];
 #pragma unroll
-    for (int j = 0; j < VT; ++j) o[j] = v4f{0.f, 0.f, 0.f, 0.f};
+    for (int r = 0; r < R; ++r) {
+        M[r] = kNothing, l[r] = 0.f;
+        weights[r] = v4f{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int j = 0; j < VT; ++j) o[r][j] = v4f{0.f, 0.f, 0.f, 0.f};
+    }
     const v8h ones = {1, 1, 1, 1, 1, 1, 1, 1};
 
     const uint32_t tiles = (limit + kKeysPerTile - 1) / kKeysPerTile;
@@ -215,22 +239,26 @@ __global__ __launch_bounds__(kWaves *kWave, D == 256 ? 2 : 4) void tree_attentio
     if (tile_1 < tiles) request(tile_1, 1, number_1);
 
     // query rows: channels (D / 4) q .. of this lane's row, in the order the nibbles come in
-    v8h qf[KD];
-    const int row = row0 + l16, new_row_of = row / a.group;
-    const bool there = row < rows;
-    const uint64_t word = there && a.mask ? a.mask[first + new_row_of] : 0;
-    float bias;
-    {
-        const __half *src = a.Q + (there ? (first + new_row_of) * a.ldq + (h * a.group + row - new_row_of * a.group) * D : first * a.ldq) + q * (D / 4);
+    v8h qf[R][KD];
+    int new_row_of[R];
+    uint64_t word[R];
+    float bias[R];
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        const int row = row0 + 16 * r + l16, of = row / a.group;
+        const bool there = row < rows;
+        new_row_of[r] = of;
+        word[r] = there && a.mask ? a.mask[first + of] : 0;
+        const __half *src = a.Q + (there ? (first + of) * a.ldq + (h * a.group + row - of * a.group) * D : first * a.ldq) + q * (D / 4);
         float sum = 0.f;
 #pragma unroll
         for (int d = 0; d < KD; ++d) {
             const v8h x = *reinterpret_cast<const v8h *>(src + 8 * d);
 #pragma unroll
             for (int e = 0; e < 8; ++e) sum += (float)x[e];
-            qf[d] = v8h{x[0], x[4], x[1], x[5], x[2], x[6], x[3], x[7]};
+            qf[r][d] = v8h{x[0], x[4], x[1], x[5], x[2], x[6], x[3], x[7]};
         }
-        bias = -8.f * 0x1p-20f * quarter_sum(sum);
+        bias[r] = -8.f * 0x1p-20f * quarter_sum(sum);
     }
 
     while (tile < tiles) {
@@ -257,24 +285,27 @@ __global__ __launch_bounds__(kWaves *kWave, D == 256 ? 2 : 4) void tree_attentio
         const uint32_t tile_3 = following(tile_2);
         pages_of(tile_3, number_2);
 
-        v4f s[2];
+        v4f s[R][2];
 #pragma unroll
-        for (int f = 0; f < 2; ++f) s[f] = v4f{bias, bias, bias, bias};
+        for (int r = 0; r < R; ++r)
+#pragma unroll
+            for (int f = 0; f < 2; ++f) s[r][f] = v4f{bias[r], bias[r], bias[r], bias[r]};
 #pragma unroll
         for (int d = 0; d < KD; ++d)
 #pragma unroll
             for (int f = 0; f < 2; ++f) {
                 const uint32_t x = kx[f][d];
                 const v4i w = {(int)((x << 4) & 0x00F000F0u), (int)(x & 0x00F000F0u), (int)((x >> 4) & 0x00F000F0u), (int)((x >> 8) & 0x00F000F0u)};
-                s[f] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(v8h, w), qf[d], s[f], 0, 0, 0);
+#pragma unroll
+                for (int r = 0; r < R; ++r) s[r][f] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(v8h, w), qf[r][d], s[r][f], 0, 0, 0);
             }
         // scores times steps (the mixed-precision multiply-add takes the fp16 as it is); keys that a row does not see
-        float step_v[8], step_log[8];                  // fp32 bits as a number: 2^23 (127 + log2), to within 0.09 2^23 below
+        float step_v[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
             step_v[e] = (float)vs[e / 4][e % 4];
-            step_log[e] = (float)__builtin_bit_cast(int, step_v[e]);
-            s[e / 4][e % 4] = __builtin_fmaf(s[e / 4][e % 4], (float)ks[e / 4][e % 4], 0.f);
+#pragma unroll
+            for (int r = 0; r < R; ++r) s[r][e / 4][e % 4] = __builtin_fmaf(s[r][e / 4][e % 4], (float)ks[e / 4][e % 4], 0.f);
         }
         const uint32_t key0 = tile * kKeysPerTile;
         if (key0 + kKeysPerTile > all_see || !ok[0] || !ok[NP - 1]) {
@@ -282,35 +313,61 @@ __global__ __launch_bounds__(kWaves *kWave, D == 256 ? 2 : 4) void tree_attentio
             for (int e = 0; e < 8; ++e) {
                 const uint32_t key = key0 + 16 * (e / 4) + 4 * q + e % 4;
                 const int new_key = (int)(key - past);
-                const bool written = (key < limit) & ok[e / 4 % NP], by_mask = (word >> (new_key & 63)) & 1, by_order = new_key <= new_row_of;
-                const bool sees = written & ((key < past) | (a.mask ? by_mask : by_order));        // no branches
-                if (!written) step_v[e] = step_log[e] = 0.f;
-                s[e / 4][e % 4] = sees ? s[e / 4][e % 4] : -INFINITY;
+                const bool written = (key < limit) & ok[e / 4 % NP];
+                if (!written) step_v[e] = 0.f;
+#pragma unroll
+                for (int r = 0; r < R; ++r) {
+                    const bool by_mask = (word[r] >> (new_key & 63)) & 1, by_order = new_key <= new_row_of[r];
+                    const bool sees = written & ((key < past) | (a.mask ? by_mask : by_order));    // no branches
+                    s[r][e / 4][e % 4] = sees ? s[r][e / 4][e % 4] : -INFINITY;
+                }
             }
         }
-        float want[8], w[8];
+        float w[R][8], product[R][8];
+        bool large = false;
+        auto weigh = [&](int r) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) want[e] = __builtin_fmaf(s[e / 4][e % 4], a.score_scale * 0x1p23f, step_log[e]);
-        const float most = __builtin_fmaf(quarter_max(fmaxf(fmaxf(fmaxf(want[0], want[1]), fmaxf(want[2], want[3])),
-                                                            fmaxf(fmaxf(want[4], want[5]), fmaxf(want[6], want[7])))), 0x1p-23f, -127.f);
-        // up by what the roundings of `most` and of the exponents below may be off, which counts where scores are huge only
-        const float top = fmaxf(most, kNothing), up = __builtin_fmaf(fabsf(top), 0x1p-22f, top);
-        if (__any(up > M + 14.f)) {
-            const float M_new = fmaxf(M, up - 7.9f), fade = __builtin_amdgcn_exp2f(M - M_new);
-            M = M_new;
-            l *= fade;
-            weights *= fade;
+            for (int e = 0; e < 8; ++e) {
+                w[r][e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r][e / 4][e % 4], a.score_scale, -M[r]));
+                product[r][e] = w[r][e] * step_v[e];
+            }
+        };
 #pragma unroll
-            for (int j = 0; j < VT; ++j) o[j] *= fade;
+        for (int r = 0; r < R; ++r) {
+            weigh(r);
+            const float most = fmaxf(fmaxf(fmaxf(product[r][0], product[r][1]), fmaxf(product[r][2], product[r][3])),
+                                     fmaxf(fmaxf(product[r][4], product[r][5]), fmaxf(product[r][6], product[r][7])));
+            large = large | (most > 0x1p14f);
         }
-        v8h p;
+        if (__any(large)) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            w[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e / 4][e % 4], a.score_scale, -M));
-            p[e] = (_Float16)(w[e] * step_v[e]);
+            for (int r = 0; r < R; ++r) {
+                float top = kNothing;                  // the row's largest score plus logarithm of the step
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const float log = fmaxf(__builtin_fmaf((float)__builtin_bit_cast(int, step_v[e]), 0x1p-23f, -127.f), -25.f);
+                    top = fmaxf(top, __builtin_fmaf(s[r][e / 4][e % 4], a.score_scale, log));
+                }
+                top = quarter_max(top);
+                // up by what the roundings of `top` and of the exponents may be off, which counts where scores are huge only
+                top = __builtin_fmaf(fabsf(top), 0x1p-22f, top);
+                const float M_new = fmaxf(M[r], top - 7.9f), fade = __builtin_amdgcn_exp2f(M[r] - M_new);
+                M[r] = M_new;
+                l[r] *= fade;
+                weights[r] *= fade;
+#pragma unroll
+                for (int j = 0; j < VT; ++j) o[r][j] *= fade;
+                weigh(r);
+            }
         }
-        l += ((w[0] + w[1]) + (w[2] + w[3])) + ((w[4] + w[5]) + (w[6] + w[7]));
-        weights = __builtin_amdgcn_mfma_f32_16x16x32_f16(ones, p, weights, 0, 0, 0);
+        v8h p[R];
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) p[r][e] = (_Float16)product[r][e];
+            l[r] += ((w[r][0] + w[r][1]) + (w[r][2] + w[r][3])) + ((w[r][4] + w[r][5]) + (w[r][6] + w[r][7]));
+            weights[r] = __builtin_amdgcn_mfma_f32_16x16x32_f16(ones, p[r], weights[r], 0, 0, 0);
+        }
         // values: unit lane % 16 of eight keys, two keys of one channel to a dword
 #pragma unroll
         for (int i = 0; i < D / 32; ++i) {
@@ -324,8 +381,11 @@ __global__ __launch_bounds__(kWaves *kWave, D == 256 ? 2 : 4) void tree_attentio
                 even[d] = (int)((t << 4) & 0x00F000F0u);
                 odd[d] = (int)(t & 0x00F000F0u);
             }
-            o[2 * i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(v8h, even), p, o[2 * i], 0, 0, 0);
-            o[2 * i + 1] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(v8h, odd), p, o[2 * i + 1], 0, 0, 0);
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+                o[r][2 * i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(v8h, even), p[r], o[r][2 * i], 0, 0, 0);
+                o[r][2 * i + 1] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(v8h, odd), p[r], o[r][2 * i + 1], 0, 0, 0);
+            }
         }
         tile = tile_1;
         tile_1 = tile_2;
@@ -339,10 +399,11 @@ __global__ __launch_bounds__(kWaves *kWave, D == 256 ? 2 : 4) void tree_attentio
     }
     __syncthreads();                                   // the ring becomes the place where the sums meet
 
-    // the waves' sums meet, CB channels at a time
-    {
-        const float sum = quarter_sum(l);
-        if (q == 0) meet_ml[wave][l16] = float2{M, sum};
+    // the waves' sums meet, 16 rows and CB channels at a time
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        const float sum = quarter_sum(l[r]);
+        if (q == 0) meet_ml[wave][l16] = float2{M[r], sum};
 #pragma unroll
         for (int cb = 0; cb < D / CB; ++cb) {
             if (q * (D / 4) / CB == cb) {
@@ -350,15 +411,15 @@ __global__ __launch_bounds__(kWaves *kWave, D == 256 ? 2 : 4) void tree_attentio
                 for (int e = 0; e < 4; ++e)
 #pragma unroll
                     for (int j = 0; j < VT; j += 4) {
-                        const float off = -8.f * weights[e];
+                        const float off = -8.f * weights[r][e];
                         *reinterpret_cast<float4 *>(&meet[wave][l16][q * (D / 4) % CB + e * VT + j]) =
-                            float4{__builtin_fmaf(o[j][e], 0x1p20f, off), __builtin_fmaf(o[j + 1][e], 0x1p20f, off),
-                                   __builtin_fmaf(o[j + 2][e], 0x1p20f, off), __builtin_fmaf(o[j + 3][e], 0x1p20f, off)};
+                            float4{__builtin_fmaf(o[r][j][e], 0x1p20f, off), __builtin_fmaf(o[r][j + 1][e], 0x1p20f, off),
+                                   __builtin_fmaf(o[r][j + 2][e], 0x1p20f, off), __builtin_fmaf(o[r][j + 3][e], 0x1p20f, off)};
                     }
             }
             __syncthreads();
             constexpr int PER = CB / 16;                               // channels per thread
-            const int mine = threadIdx.x / 16, at = (threadIdx.x % 16) * PER, row = row0 + mine;
+            const int mine = threadIdx.x / 16, at = (threadIdx.x % 16) * PER, row = row0 + 16 * r + mine;
             if (row < rows) {
                 float top = kNothing, total = 0.f, out[PER] = {};
 #pragma unroll
@@ -450,12 +511,12 @@ __global__ __launch_bounds__(256) void tree_attention_join_kernel(const CacheVie
     *reinterpret_cast<v4hs *>(a.O + (first + i) * a.ldo + hq * D + 4 * mine) = y;
 }
 
-template <int D, bool ONE_PAGE>
+template <int D, bool ONE_PAGE, int R>
 sq_status launch_tree_attention(const CacheView &c, const AttentionCall &a, hipStream_t st)
 {
     const int64_t blocks = (int64_t)a.row_blocks * a.splits * c.Hk * c.B;
     if (blocks > 0x7FFFFFFF) return SQ_ERR_SHAPE;
-    hipLaunchKernelGGL((tree_attention_kernel<D, ONE_PAGE>), dim3((unsigned)blocks), dim3(kWaves * kWave), 0, st, c, a);
+    hipLaunchKernelGGL((tree_attention_kernel<D, ONE_PAGE, R>), dim3((unsigned)blocks), dim3(kWaves * kWave), 0, st, c, a);
     if (hipGetLastError() != hipSuccess) return SQ_ERR_LAUNCH;
     if (a.splits == 1) return SQ_OK;
     const int64_t units = (int64_t)a.max_rows * a.Hq;
@@ -470,13 +531,14 @@ sq_status dispatch_tree_attention(const CacheView &c, AttentionCall &a, int64_t 
 {
     const int64_t rows = (int64_t)a.max_rows * a.group;
     if (rows > (1 << 30)) return SQ_ERR_SHAPE;
-    a.row_blocks = (int)((rows + 15) / 16);
-    // As many splits as keep the workgroups within the four that a CU holds (a few more would make a second round), chunks of
-    // at least 128 keys, and what the workspace holds.  (us at 48 sequences of 8192 keys, 8 heads: two splits, 768 workgroups,
-    // 95; three, 1152 of them, 111; 16 trees, 1536 workgroups without a split 107, with two 151.)
+    const int64_t per_block = D < 256 && rows > 16 ? 32 : 16;
+    a.row_blocks = (int)((rows + per_block - 1) / per_block);
+    // As many splits as keep the workgroups within the four (R = 2: two) that a CU holds (a few more would make a second
+    // round), chunks of at least 128 keys, and what the workspace holds.  (us at 48 sequences of 8192 keys, 8 heads: two splits, 768 workgroups,
+    // 95; three, 1152 of them, 111; 16 trees, 1536 workgroups of 16 rows without a split 107, with two 151.)
     const int64_t units = (int64_t)a.row_blocks * c.Hk * c.B;
     max_keys = max_keys < 1 ? 1 : max_keys;
-    int64_t splits = 1024 / units;
+    int64_t splits = (per_block == 32 ? 512 : 1024) / units;
     const int64_t chunks = (max_keys + kChunkUnit - 1) / kChunkUnit, room = workspace_bytes / (a.T * a.Hq * (D + 2) * 4);
     splits = splits < chunks ? splits : chunks;
     splits = splits < kMaxSplits ? splits : kMaxSplits;
@@ -484,7 +546,9 @@ sq_status dispatch_tree_attention(const CacheView &c, AttentionCall &a, int64_t 
     a.splits = splits < 1 ? 1 : (int)splits;
     a.part = static_cast<float *>(workspace);
     a.tiles_per_chunk = kWaves * (int)((chunks + a.splits - 1) / a.splits);
-    return c.page_shift > 4 ? launch_tree_attention<D, true>(c, a, st) : launch_tree_attention<D, false>(c, a, st);
+    if constexpr (D < 256)
+        if (per_block == 32) return c.page_shift > 4 ? launch_tree_attention<D, true, 2>(c, a, st) : launch_tree_attention<D, false, 2>(c, a, st);
+    return c.page_shift > 4 ? launch_tree_attention<D, true, 1>(c, a, st) : launch_tree_attention<D, false, 1>(c, a, st);
 }
 
 }  // namespace
