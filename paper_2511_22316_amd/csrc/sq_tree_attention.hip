@@ -88,7 +88,7 @@ __device__ __forceinline__ int by_length(const CacheView &c, const AttentionCall
 // A workgroup takes one head of K and V of one sequence, 16 R query rows (row = new row * group + query head in the group)
 // and every splits-th chunk of its keys; its four waves take every fourth tile of 32 keys each and work alone until
 // the end.  What it does per key, whatever the rows, is most of the work of 16 of them (widening the codes: 120 of 260
-// instructions), so more than 16 rows are taken 32 at a time (R = 2), at half the waves per SIMD: the trees above 116 -> 94 us,
+// instructions), so more rows are taken 32 at a time (R = 2) where there is enough to do, at half the waves per SIMD: the trees above 116 -> 94 us,
 // prompts of 256 to 512 rows 189 -> 128.  Neighbouring workgroups belong to an XCD and have a head of many sequences.
 //
 // Scores: S^T = K Q^T on v_mfma_f32_16x16x32_f16, the keys as rows of the result and the query rows as columns, so a lane has
@@ -531,13 +531,17 @@ sq_status dispatch_tree_attention(const CacheView &c, AttentionCall &a, int64_t 
 {
     const int64_t rows = (int64_t)a.max_rows * a.group;
     if (rows > (1 << 30)) return SQ_ERR_SHAPE;
-    const int64_t per_block = D < 256 && rows > 16 ? 32 : 16;
+    max_keys = max_keys < 1 ? 1 : max_keys;
+    // 32 rows per workgroup from about two waves of work for every SIMD on (us, 16 / 32: 16 sequences, 20 rows, 1024 keys 16.8 /
+    // 18.6; one prompt of 300 rows 13.2 / 15.3; 16 sequences, 32 rows, 4096 keys 30.5 / 30.7; one tree of 61 new rows, 16384 keys
+    // 44.7 / 39.9; 64 sequences, 28 rows, 8192 keys 122.7 / 103.2).  256 channels of two tiles of rows do not fit in registers.
+    const int64_t blocks_of_16 = (rows + 15) / 16 * c.Hk * c.B;
+    const int64_t per_block = D < 256 && rows > 16 && (double)blocks_of_16 * (double)max_keys > 0x1p20 ? 32 : 16;
     a.row_blocks = (int)((rows + per_block - 1) / per_block);
     // As many splits as keep the workgroups within the four (R = 2: two) that a CU holds (a few more would make a second
     // round), chunks of at least 128 keys, and what the workspace holds.  (us at 48 sequences of 8192 keys, 8 heads: two splits, 768 workgroups,
     // 95; three, 1152 of them, 111; 16 trees, 1536 workgroups of 16 rows without a split 107, with two 151.)
     const int64_t units = (int64_t)a.row_blocks * c.Hk * c.B;
-    max_keys = max_keys < 1 ? 1 : max_keys;
     int64_t splits = (per_block == 32 ? 512 : 1024) / units;
     const int64_t chunks = (max_keys + kChunkUnit - 1) / kChunkUnit, room = workspace_bytes / (a.T * a.Hq * (D + 2) * 4);
     splits = splits < chunks ? splits : chunks;

@@ -581,3 +581,82 @@ def test_decode_step_of_all_operators_captured():
                 ou.held(got_o.reshape(B, Hq, D)[b, h][None], want, ob, f"step {i}: attention")
         want, yb = ou.product(got_o, codes[1][0].reshape(Kin, Hq * D), codes[1][1], group)
         ou.held(got_y, want, yb, f"step {i}: output")
+
+
+MANY_KEYS = 2 ** 31 - 1                                     # as a hint: the work is shared out as for long sequences, 32 rows at a time
+
+
+@pytest.mark.parametrize("case", [n for n, c in enumerate(CASES) if max(c[1]) * (c[2] // c[3]) > 16])
+def test_attention_of_many_rows(case):
+    past, new, Hq, Hk, D, page, tree = CASES[case]
+    print(f"case attention many rows {CASES[case]}", flush=True)
+    s = Setting(700 + case, past, new, Hk, D, page, scale_v=[1.0, 2.0 ** -12, 8.0][case % 3])
+    Q, scale = s.queries(Hq, 2.0), D ** -0.5
+    words = s.trees() if tree else None
+    want, bound = s.expect(Q, Hq // Hk, s.by_mask(words) if tree else s.causal, scale)
+    for workspace in (0, 8 << 20):
+        ou.held(s.run(Q, words, scale, workspace, max_keys=MANY_KEYS), want, bound, f"{CASES[case]} {workspace}")
+
+
+def test_attention_of_many_rows_empty_ones_bad_pages_and_peaks():
+    print("case attention many rows, masks and pages", flush=True)
+    for D, page in ((64, 16), (128, 32)):
+        s = Setting(800 + D, [0, 170, 0], [40, 19, 1], 2, D, page)
+        words = s.trees()
+        words[::3] = 0
+        words[7] = np.uint64(1) << np.uint64(63)
+        words[41] = np.uint64(0xFFFFFFFFFFFFFFFF)
+        Q = s.queries(8, 3.0)
+        want, bound = s.expect(Q, 4, s.by_mask(words), 0.125)
+        got = s.run(Q, words, 0.125, max_keys=MANY_KEYS)
+        ou.held(got, want, bound, "empty rows")
+        assert (got[0] == 0).all() and (got[7] == 0).all()
+        table = s.table.copy()
+        table[1, 2], table[1, 4], table[0, :] = -1, 1 << 30, s.cache.shape[0]
+        absent = lambda b, L: np.ones(L, bool) if b == 0 else np.isin(np.arange(L) // page, (2, 4)) & (b == 1)    # noqa: E731
+        want, bound = s.expect(Q, 4, s.by_mask(words), 0.125, absent)
+        got = s.run(Q, words, 0.125, max_keys=MANY_KEYS, table=table)
+        ou.held(got, want, bound, "bad pages")
+        assert (got[:40] == 0).all()
+        for factor in (30.0, 300.0):                        # one key with all the weight; the offset moves on the way
+            Q = s.queries(8, factor)
+            want, bound = s.expect(Q, 4, s.causal, 0.3)
+            ou.held(s.run(Q, None, 0.3, max_keys=MANY_KEYS), want, bound, f"{factor}")
+
+
+@pytest.mark.parametrize("B", [64, 65])
+def test_attention_of_many_rows_in_many_sequences(B):
+    """Sequences of equal and of different lengths, some without a row."""
+    print(f"case attention many rows {B} sequences", flush=True)
+    g = rng(12, B)
+    past, new = g.integers(0, 60, B), g.integers(0, 12, B)
+    past[10:20], new[10:20] = 33, 9
+    s = Setting(900 + B, list(past), list(new), 1, 64, 16)
+    Q = s.queries(4)
+    want, bound = s.expect(Q, 4, s.causal, 0.2)
+    ou.held(s.run(Q, None, 0.2, max_rows=12, max_keys=MANY_KEYS), want, bound, str(B))
+
+
+@pytest.mark.parametrize("B", [63, 65, 4097, 5000])
+def test_cache_of_many_sequences(B):
+    import torch
+    import paper_2511_22316_amd as sq
+    print(f"case cache {B} sequences", flush=True)
+    g, Hk, D, page = rng(13, B), 1, 64, 16
+    cached, new = g.integers(0, 15, B).astype(np.int32), g.integers(0, 3, B)
+    new[B // 3: B // 2] = 0                                 # a run of sequences that share their row_start
+    start = np.concatenate([[0], np.cumsum(new)]).astype(np.int32)
+    T = int(start[-1])
+    table = g.permutation(B).reshape(B, 1).astype(np.int32)
+    x = rows(g, T, 2 * Hk * D).reshape(T, 2, Hk, D)
+    cache = torch.zeros(B, sq.sq_cache_page_bytes(Hk, D, page), dtype=torch.uint8, device="cuda")
+    args = dev(start), dev(cached), dev(table), page
+    d = dev(x)
+    sq.sq_cache_append(d[:, 0], d[:, 1], *args, cache)
+    k, v = (torch.full((T, Hk, D), 3.0, dtype=torch.float16, device="cuda") for _ in range(2))
+    sq.sq_cache_read(cache, *args, k, v)
+    codes, steps = ou.quantize(x)
+    want = (codes * steps.astype(np.float64)[..., None]).astype(np.float16).reshape(x.shape)
+    place = np.repeat(cached, new) + np.arange(T) - np.repeat(start[:-1], new)
+    want[place >= page] = 3.0                               # rows beyond a sequence's page
+    assert np.array_equal(host(k), want[:, 0]) and np.array_equal(host(v), want[:, 1])
