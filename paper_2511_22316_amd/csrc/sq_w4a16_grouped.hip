@@ -410,26 +410,40 @@ sq_status launch_grouped_rows(const GroupedArgs &a)
 template <int GROUP>
 sq_status launch_grouped_few(const GroupedArgs &a)
 {
-    if (a.T <= 16 && a.K % 128 == 0 && a.T * (int64_t)(2 * a.K + kRowPad) <= kMaxDynamicLds && (int64_t)a.K * a.N >= ((int64_t)32 << 20))
+    const int64_t tiles = (a.T + 15) / 16, blocks = (a.N + 15) / 16;
+    // Token rows in LDS where they fit and there is enough to share out evenly (us, that / the other kernel at its best, T = 1,
+    // groups of 128: K = 4096, N = 8192 9.0 / 7.7, N = 9216 10.3 / 12.0; K = 8192, N = 8192 12.7 / 13.7, N = 28672 28.9 / 38.0), at
+    // more than one block of channels per workgroup (K = 11008, N = 4096 10.9 / 10.1).
+    if (tiles == 1 && a.K % 128 == 0 && a.T * (int64_t)(2 * a.K + kRowPad) <= kMaxDynamicLds && blocks > 256 && (int64_t)a.K * a.N > ((int64_t)32 << 20))
         return launch_grouped_rows<GROUP, 8, 4>(a);
-    const int tiles = (a.T + 15) / 16, blocks = (a.N + 15) / 16;
-    if (tiles == 2 && blocks / 4 >= 170) return launch_grouped_skinny<GROUP, 4, 8, 2, 1>(a);
-    if (blocks / 4 * tiles >= 170) return launch_grouped_skinny<GROUP, 4, 8, 1, GROUP <= 64 ? 1 : 2>(a);
-    if (blocks / 2 * tiles >= 170) return launch_grouped_skinny<GROUP, 2, 8, 1, 2>(a);
-    return launch_grouped_skinny<GROUP, 1, 8, 1, 2>(a);
+    // The fewest channels per workgroup that need one round of workgroups on the 256 CUs (us with 16 / 32 / 64 channels, T = 1,
+    // K = 4096, groups of 128: N = 4096 5.8 / 7.4 / 11.8, N = 6144 9.0 / 7.5 / 12.0, N = 9216 12.2 / 12.7 / 12.0), and both blocks of
+    // 16 tokens in a workgroup before there are two rounds (T = 32, N = 11008 26.0 / 19.8).  Groups of 32 and 64 have more
+    // registers of steps: a slice at a time then fits.
+    if (blocks * tiles <= 256) return launch_grouped_skinny<GROUP, 1, 8, 1, 2>(a);
+    if (blocks * tiles <= 512) return launch_grouped_skinny<GROUP, 2, 8, 1, 2>(a);
+    if (tiles == 1 || blocks * tiles <= 1024) return launch_grouped_skinny<GROUP, 4, 8, 1, GROUP <= 64 ? 1 : 2>(a);
+    return launch_grouped_skinny<GROUP, 4, 8, 2, 1>(a);
 }
 
-// Many tokens: the tile kernel of sq_w4a16_gemm with the steps on the widened codes, in its shapes and by its rules.
+// Many tokens: the tile kernel of sq_w4a16_gemm with the steps on the widened codes.  Us per shape, groups of 128:
+//   64 x 128, two K groups    T = 333, K = N = 4096 26; up to 64 tokens in any case (K = 8192, N = 57344 108)
+//   128 x 128, two K groups   T = 333, K = N = 4096 33; T = 333, N = 9000 38.5 (64 x 128 45.6); T = 1000, N = 4096 44 (53)
+//   128 x 256                 T = 333, K = N = 4096 47; T = 600, N = 9000 56 (128 x 128 73); T = 64, K = 8192, N = 57344 120
+//   256 x 256                 1.85 times as long per round of 256 workgroups as 128 x 256, over seven shapes, so it is taken where
+//                             that is less: T = 4096, K = 11008, N = 4096 351 (389), T = 1500, K = 4096, N = 14336 218 (184)
+// T = 2048, K = N = 4096 takes 70 us (groups of 32 77; one step per channel 67), T = 333, K = 5120, N = 13824 66 (74; 61).
 sq_status launch_grouped_many(const GroupedArgs &a)
 {
     const int shift = __builtin_ctz((unsigned)a.group);
-    const int64_t tiles_64x128 = ((int64_t)a.T + 63) / 64 * (((int64_t)a.N + 127) / 128), tiles_128 = ((int64_t)a.T + 127) / 128 * (((int64_t)a.N + 127) / 128);
-    const int64_t tiles_large = ((int64_t)a.T + 255) / 256 * (((int64_t)a.N + 255) / 256);
-    if (a.K % 128 == 0 && tiles_64x128 <= 256)
+    auto tiles = [&](int bm, int bn) { return ((int64_t)a.T + bm - 1) / bm * (((int64_t)a.N + bn - 1) / bn); };
+    auto rounds = [&](int bm, int bn) { return (tiles(bm, bn) + 255) / 256; };
+    const bool two_k_groups = a.K % 128 == 0;
+    if (two_k_groups && (a.T <= 64 || tiles(64, 128) <= 256))
         return launch_w4a16_ring<1, 4, 2, 1, 1, 64, 0, 2, true>(a.X, a.ldx, a.T, a.K, a.Qw, a.steps, a.N, a.Y, a.ldy, a.st, shift);
-    if (a.K % 128 == 0 && tiles_128 <= 256)
+    if (two_k_groups && tiles(128, 128) <= 256)
         return launch_w4a16_ring<1, 4, 4, 1, 1, 64, 0, 2, true>(a.X, a.ldx, a.T, a.K, a.Qw, a.steps, a.N, a.Y, a.ldy, a.st, shift);
-    if (tiles_large >= 192)
+    if (37 * rounds(256, 256) < 20 * rounds(128, 256))
         return launch_w4a16_ring<2, 4, 4, 2, 1, 64, 0, 1, true>(a.X, a.ldx, a.T, a.K, a.Qw, a.steps, a.N, a.Y, a.ldy, a.st, shift);
     return launch_w4a16_ring<1, 4, 4, 2, 1, 64, 4, 1, true>(a.X, a.ldx, a.T, a.K, a.Qw, a.steps, a.N, a.Y, a.ldy, a.st, shift);
 }
@@ -450,6 +464,8 @@ extern "C" sq_status sq_w4a16_gemm_grouped(const void *X, int64_t T, int32_t K, 
         return SQ_ERR_ALIGN;
     const sq::GroupedArgs a = {static_cast<const __half *>(X), ldx, (int)T, K, Qw, static_cast<const __half *>(steps), group, N,
                                static_cast<__half *>(Y), ldy, static_cast<hipStream_t>(stream)};
+    // (From 17 tokens on the tiles would be the faster ones where the pass over the codes takes two rounds of workgroups, T = 32,
+    // K = 4096, N = 22016 28.4 us for 37.0, but they round every weight to fp16: up to 32 tokens keep theirs as they are.)
     if (T > 32) return sq::launch_grouped_many(a);
     if (group == 32) return sq::launch_grouped_few<32>(a);
     if (group == 64) return sq::launch_grouped_few<64>(a);

@@ -660,3 +660,15 @@ def test_cache_of_many_sequences(B):
     place = np.repeat(cached, new) + np.arange(T) - np.repeat(start[:-1], new)
     want[place >= page] = 3.0                               # rows beyond a sequence's page
     assert np.array_equal(host(k), want[:, 0]) and np.array_equal(host(v), want[:, 1])
+
+
+@pytest.mark.parametrize("T,K,N,group", [(1, 256, 4200, 128), (16, 448, 8190, 64), (9, 192, 5000, 32), (20, 256, 4200, 32), (32, 320, 8300, 64),
+                                         (17, 256, 11000, 128), (32, 192, 9000, 32), (29, 512, 16384, 256), (20, 256, 16500, 128),
+                                         (32, 64, 17000, 32), (40, 256, 33000, 64), (1000, 256, 2500, 32), (300, 128, 9000, 128)])
+def test_product_of_many_channels(T, K, N, group):
+    """More channels, where the choice of a kernel goes by them."""
+    print(f"case product {T} {K} {N} {group}", flush=True)
+    g = rng(14, T, K, N, group)
+    X, (codes, steps) = rows(g, T, K), weights(g, N, K, group)
+    want, bound = ou.product(X, codes, steps, group, T > 32)
+    ou.held(run_product(X, codes, steps, 8, 3), want, bound, f"{T} {K} {N} {group}")
