@@ -437,7 +437,8 @@ sq_status sq_quantize_grouped(const void *X, int64_t T, int32_t K, int64_t ldx,
  *
  *   X        device, fp16 [T, ldx]; rows 16-byte aligned (ldx % 8 == 0), ldx >= K
  *   Qw       device, uint8 [N, K/2], 16-byte aligned
- *   steps    device, fp16 [N, K / group], group 32, 64, 128 or 256
+ *   steps    device, fp16 [N, K / group], group 32, 64, 128 or 256; 4-byte aligned
+ *            with groups of 32
  *   Y        device out, fp16 [T, ldy], ldy >= N
  * Requires K % 64 == 0, K % group == 0, K <= 131072, T <= 2^24.  T == 0 or N == 0
  * is legal and enqueues nothing.

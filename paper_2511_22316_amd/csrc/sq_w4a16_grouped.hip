@@ -432,7 +432,8 @@ sq_status launch_grouped_few(const GroupedArgs &a)
 //   128 x 256                 T = 333, K = N = 4096 47; T = 600, N = 9000 56 (128 x 128 73); T = 64, K = 8192, N = 57344 120
 //   256 x 256                 1.85 times as long per round of 256 workgroups as 128 x 256, over seven shapes, so it is taken where
 //                             that is less: T = 4096, K = 11008, N = 4096 351 (389), T = 1500, K = 4096, N = 14336 218 (184)
-// T = 2048, K = N = 4096 takes 70 us (groups of 32 77; one step per channel 67), T = 333, K = 5120, N = 13824 66 (74; 61).
+// T = 2048, K = N = 4096 takes 74.5 us with groups of 32 or 64 (sq_w4a16_gemm with its step per channel 65), T = 333, K = 5120,
+// N = 13824 69 (60): what the steps cost is the packed multiplication per two codes and power.
 sq_status launch_grouped_many(const GroupedArgs &a)
 {
     const int shift = __builtin_ctz((unsigned)a.group);
@@ -460,7 +461,7 @@ extern "C" sq_status sq_w4a16_gemm_grouped(const void *X, int64_t T, int32_t K, 
     if (T > (1 << 24) || ldx < K || ldy < N) return SQ_ERR_SHAPE;
     if (T == 0 || N == 0) return SQ_OK;
     if (!X || !Qw || !steps || !Y) return SQ_ERR_NULL;
-    if (((uintptr_t)X & 15) || (ldx % 8) != 0 || ((uintptr_t)Qw & 15) || ((uintptr_t)Y & 1) || ((uintptr_t)steps & 1))
+    if (((uintptr_t)X & 15) || (ldx % 8) != 0 || ((uintptr_t)Qw & 15) || ((uintptr_t)Y & 1) || ((uintptr_t)steps & (group == 32 ? 3 : 1)))
         return SQ_ERR_ALIGN;
     const sq::GroupedArgs a = {static_cast<const __half *>(X), ldx, (int)T, K, Qw, static_cast<const __half *>(steps), group, N,
                                static_cast<__half *>(Y), ldy, static_cast<hipStream_t>(stream)};

@@ -84,18 +84,46 @@ __device__ __forceinline__ void dma_16_if(const void *gptr, uint32_t lds_addr, i
                  : "memory", "m0", "scc");
 }
 
-__device__ __forceinline__ void dma_2_if(const void *gptr, uint32_t lds_addr, int a, int b)
+// Two bytes, or four with groups of 32, of each of the first LANES lanes, global memory -> the dword at lds_addr + 4 lane
+// (two are zero-extended); else as dma_16_if
+template <int LANES>
+__device__ __forceinline__ void dma_step_if(const void *gptr, uint32_t lds_addr, int a, int b, int group_shift)
 {
-    // two bytes per lane, global memory -> the dword at lds_addr + 4 lane, zero-extended; else as dma_16_if
-    asm volatile("s_cmp_lt_i32 %2, %3\n\t"
-                 "s_cbranch_scc0 .Lsq2_skip_%=\n\t"
-                 "s_mov_b32 m0, %1\n\t"
-                 "s_nop 0\n\t"
-                 "global_load_lds_ushort %0, off\n"
-                 ".Lsq2_skip_%=:"
-                 :
-                 : "v"(gptr), "s"(lds_addr), "s"(a), "s"(b)
-                 : "memory", "m0", "scc");
+    static_assert(LANES == 32 || LANES == 64, "a wave or half of it");
+    if constexpr (LANES == 64)
+        asm volatile("s_cmp_lt_i32 %2, %3\n\t"
+                     "s_cbranch_scc0 .Lsqs_skip_%=\n\t"
+                     "s_mov_b32 m0, %1\n\t"
+                     "s_cmp_eq_u32 %4, 5\n\t"
+                     "s_cbranch_scc1 .Lsqs_four_%=\n\t"
+                     "global_load_lds_ushort %0, off\n\t"
+                     "s_branch .Lsqs_skip_%=\n"
+                     ".Lsqs_four_%=:\n\t"
+                     "global_load_lds_dword %0, off\n"
+                     ".Lsqs_skip_%=:"
+                     :
+                     : "v"(gptr), "s"(lds_addr), "s"(a), "s"(b), "s"(group_shift)
+                     : "memory", "m0", "scc");
+    else {
+        uint32_t upper;
+        asm volatile("s_cmp_lt_i32 %3, %4\n\t"
+                     "s_cbranch_scc0 .Lsqs_skip_%=\n\t"
+                     "s_mov_b32 m0, %2\n\t"
+                     "s_mov_b32 %0, exec_hi\n\t"
+                     "s_mov_b32 exec_hi, 0\n\t"
+                     "s_cmp_eq_u32 %5, 5\n\t"
+                     "s_cbranch_scc1 .Lsqs_four_%=\n\t"
+                     "global_load_lds_ushort %1, off\n\t"
+                     "s_branch .Lsqs_done_%=\n"
+                     ".Lsqs_four_%=:\n\t"
+                     "global_load_lds_dword %1, off\n"
+                     ".Lsqs_done_%=:\n\t"
+                     "s_mov_b32 exec_hi, %0\n"
+                     ".Lsqs_skip_%=:"
+                     : "=&s"(upper)
+                     : "v"(gptr), "s"(lds_addr), "s"(a), "s"(b), "s"(group_shift)
+                     : "memory", "m0", "scc");
+    }
 }
 
 // Tile kernel for many tokens.  Block tile (WM FM 32) tokens x (WN FN 32) channels, WM x WN waves
@@ -124,8 +152,9 @@ __device__ __forceinline__ void dma_2_if(const void *gptr, uint32_t lds_addr, in
 // LW > 0: LW more waves that only request the tiles and wait for them; the multiplying waves then
 // issue no memory instruction inside the loop and meet the others at the barrier of each tile.
 // KG: groups of WM WN waves that walk K / KG elements each, through rings of their own, and add their sums through LDS.
-// GROUPED: a step per group of 1 << group_shift >= 32 elements of K in place of one per channel.  The steps of a tile's two
-// halves travel with it (a dword each), and a widened code is multiplied by its step in fp16, rounded once: a lane's 32
+// GROUPED: a step per group of 1 << group_shift >= 32 elements of K in place of one per channel.  The step of a tile, or the
+// two of its halves, travel with it (a dword per channel; each is of another row, and their number is what these loads cost:
+// with a load per half T = 333, K = 5120, N = 13824, groups of 32 took 73.5 us, so 69.3), and a widened code is multiplied by its step in fp16, rounded once: a lane's 32
 // elements of a tile lie in one group, so that is one packed multiplication per two codes (four widening instructions
 // instead of three).  Scaling the sums instead would keep them exact, but wants as many registers again as the sums have.
 template <int WM, int WN, int FM, int FN, int OCC, int BK, int LW, int KG, bool GROUPED>
@@ -141,13 +170,13 @@ __global__ __launch_bounds__((KG * WM * WN + LW) * kWave, OCC) void w4a16_gemm_r
     constexpr int A_ROW = 2 * BK, B_ROW = BK / 2;            // bytes of a tile row
     constexpr int A_CPR = A_ROW / 16, B_CPR = B_ROW / 16;    // 16-byte chunks per row
     constexpr int A_RPL = 64 / A_CPR, B_RPL = 64 / B_CPR;    // rows filled by one wave-wide load
-    constexpr int A_BYTES = BM * A_ROW, B_BYTES = BN * B_ROW, S_BYTES = GROUPED ? 2 * BN * 4 : 0;
+    constexpr int A_BYTES = BM * A_ROW, B_BYTES = BN * B_ROW, S_BYTES = GROUPED ? BN * 4 : 0;
     constexpr int STAGE = A_BYTES + B_BYTES + S_BYTES;
     constexpr int NL = LW > 0 ? LW : NW;                     // waves that share the loads of a tile
     constexpr int A_LOADS = BM / A_RPL / NL, B_LOADS = BN / B_RPL / NL;       // wave-wide loads per loading wave and tile
-    constexpr int S_LOADS = GROUPED ? 2 * BN / kWave / NL : 0;
+    constexpr int S_LOADS = GROUPED ? 1 : 0, S_LANES = BN / NL;
     constexpr int LOADS = A_LOADS + B_LOADS + S_LOADS;
-    static_assert((BM / A_RPL) % NL == 0 && (BN / B_RPL) % NL == 0 && (!GROUPED || 2 * BN / kWave % NL == 0),
+    static_assert((BM / A_RPL) % NL == 0 && (BN / B_RPL) % NL == 0 && (!GROUPED || S_LANES == 32 || S_LANES == 64),
                   "loads must split evenly over the waves");
     extern __shared__ uint4 ring[];
 
@@ -186,13 +215,9 @@ __global__ __launch_bounds__((KG * WM * WN + LW) * kWave, OCC) void w4a16_gemm_r
         const int r = B_RPL * (wave + NL * u) + lane / B_CPR;
         b_src[u] = Qw + (int64_t)min(col0 + r, N - 1) * Kb + kg0 / 2 + (lane % B_CPR) * 16;
     }
-    // steps: entry BN half + channel; 64 neighbouring ones are of one half
-    const __half *s_src[GROUPED ? S_LOADS : 1];
-    if constexpr (GROUPED) {
-#pragma unroll
-        for (int u = 0; u < S_LOADS; ++u)
-            s_src[u] = sw + (int64_t)min(col0 + (kWave * (wave + NL * u) + lane) % BN, N - 1) * (K >> group_shift);
-    }
+    // steps: S_LANES channels per loading wave
+    const __half *s_src = nullptr;
+    if constexpr (GROUPED) s_src = sw + (int64_t)min(col0 + wave * S_LANES + lane % S_LANES, N - 1) * (K >> group_shift);
     const uint32_t lds_base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint4 *)ring + kg * (NS * STAGE);
     const uint32_t wave_u = __builtin_amdgcn_readfirstlane(wave);
     auto issue_tile = [&](int kt, int stage, int limit) {
@@ -202,14 +227,9 @@ __global__ __launch_bounds__((KG * WM * WN + LW) * kWave, OCC) void w4a16_gemm_r
 #pragma unroll
         for (int u = 0; u < B_LOADS; ++u)
             dma_16_if(b_src[u] + kt * (BK / 2), sa + A_BYTES + (wave_u + NL * u) * 1024, kt, limit);
-        if constexpr (GROUPED) {
-#pragma unroll
-            for (int u = 0; u < S_LOADS; ++u) {
-                const int half = kWave * ((int)wave_u + NL * u) / BN;
-                dma_2_if(s_src[u] + ((kg0 + min(kt, limit - 1) * BK + half * (BK / 2)) >> group_shift),
-                         sa + A_BYTES + B_BYTES + (wave_u + NL * u) * (4 * kWave), kt, limit);
-            }
-        }
+        if constexpr (GROUPED)
+            dma_step_if<S_LANES>(s_src + ((kg0 + min(kt, limit - 1) * BK) >> group_shift), sa + A_BYTES + B_BYTES + wave_u * (4 * S_LANES), kt, limit,
+                                 group_shift);
     };
 
     v16f acc[FM][FN];
@@ -227,7 +247,8 @@ __global__ __launch_bounds__((KG * WM * WN + LW) * kWave, OCC) void w4a16_gemm_r
     for (int s = 0; s < STEPS; ++s)
         a_off[s] = (wm * FM * 32 + l32) * A_ROW + (((STEPS * g + s) ^ ((l32 >> 1) & 7)) * 16);
     const int b_off = A_BYTES + (wn * FN * 32 + l32) * B_ROW + g * (STEPS * 4);
-    const int s_off = A_BYTES + B_BYTES + (g * BN + wn * FN * 32 + l32) * 4;
+    const int s_off = A_BYTES + B_BYTES + (wn * FN * 32 + l32) * 4;
+    const uint32_t s_half = GROUPED && group_shift == 5 && g ? 0x03020302u : 0x01000100u;       // this lane's step of the dword, twice
     const char *lds = reinterpret_cast<const char *>(ring) + kg * (NS * STAGE);
 
     uint32_t magic;                                    // 1024.0 in both halves, held in a vector register
@@ -269,7 +290,7 @@ __global__ __launch_bounds__((KG * WM * WN + LW) * kWave, OCC) void w4a16_gemm_r
         for (int j = 0; j < FN; ++j) rb[j] = *reinterpret_cast<const uint4 *>(lds + stage_byte + b_off + j * (32 * B_ROW));
         if constexpr (GROUPED) {
 #pragma unroll
-            for (int j = 0; j < FN; ++j) step2[j] = *reinterpret_cast<const uint32_t *>(lds + stage_byte + s_off + j * (32 * 4)) * 0x10001u;
+            for (int j = 0; j < FN; ++j) step2[j] = __builtin_amdgcn_perm(0u, *reinterpret_cast<const uint32_t *>(lds + stage_byte + s_off + j * (32 * 4)), s_half);
         }
     };
     auto read_tokens = [&](int set, int stage_byte, int s, int i) {
@@ -417,7 +438,7 @@ sq_status launch_w4a16_ring(const __half *X, int64_t ldx, int T, int K, const ui
                             int group_shift = 0)
 {
     constexpr int BM = WM * FM * 32, BN = WN * FN * 32;
-    constexpr size_t lds = (size_t)3 * KG * (BM * 2 * BK + BN * BK / 2 + (GROUPED ? 2 * BN * 4 : 0));
+    constexpr size_t lds = (size_t)3 * KG * (BM * 2 * BK + BN * BK / 2 + (GROUPED ? BN * 4 : 0));
     static_assert(lds <= (size_t)kMaxDynamicLds, "ring does not fit in LDS");
     auto kernel = w4a16_gemm_ring_kernel<WM, WN, FM, FN, OCC, BK, LW, KG, GROUPED>;
     if ((K % (KG * BK)) != 0) return SQ_ERR_SHAPE;
