@@ -488,8 +488,14 @@ def _heads(t, name, packed=True):
     return T, H, D, row, head
 
 
-def _here(stream):
-    return _raw_stream(_raw_device()) if stream is None else stream.cuda_stream
+def _here(stream, *tensors):
+    """The stream to work on; the tensors must be on the current device (a kernel that follows a host pointer takes the
+    process down, and sq_rotary_table's result is one that has to be copied)."""
+    device = _raw_device() if tensors[0].is_cuda else -2
+    for t in tensors:
+        if t.get_device() != device:
+            raise ValueError("tensors must be on the current device")
+    return _raw_stream(device) if stream is None else stream.cuda_stream
 
 
 def sq_quantize_grouped(X, group, Q, steps, stream=None) -> None:
@@ -502,7 +508,8 @@ def sq_quantize_grouped(X, group, Q, steps, stream=None) -> None:
         _layout(("X", X, _f16, False), ("Q", Q, _u8, True), ("steps", steps, _f16, True))
     if group <= 0 or Q.shape != (T, K // 2) or steps.shape != (T, K // group):
         raise ValueError("Q must be [T, K/2] and steps [T, K / group]")
-    code = lib.sq_quantize_grouped(X.data_ptr(), T, K, ldx if T > 1 else K, group, Q.data_ptr(), steps.data_ptr(), _here(stream))
+    code = lib.sq_quantize_grouped(X.data_ptr(), T, K, ldx if T > 1 else K, group, Q.data_ptr(), steps.data_ptr(),
+                                   _here(stream, X, Q, steps))
     if code:
         _check(code)
 
@@ -521,7 +528,7 @@ def sq_w4a16_gemm_grouped(X, Qw, steps, Y, stream=None) -> None:
     if groups <= 0 or K % groups or Qw.shape != (N, K // 2) or Y.shape != (T, N):
         raise ValueError("Qw must be [N, K/2], steps [N, K / group] and Y [T, N]")
     code = lib.sq_w4a16_gemm_grouped(X.data_ptr(), T, K, ldx if T > 1 else K, Qw.data_ptr(), steps.data_ptr(), K // groups, N,
-                                     Y.data_ptr(), ldy if T > 1 else N, _here(stream))
+                                     Y.data_ptr(), ldy if T > 1 else N, _here(stream, X, Qw, steps, Y))
     if code:
         _check(code)
 
@@ -555,7 +562,7 @@ def sq_rotary_fp16(X, positions, turns, half, Y, magnitude=1.0, stream=None) -> 
     if Y.shape != X.shape or positions.numel() != T:
         raise ValueError("Y must have the shape of X, positions one entry per token")
     code = lib.sq_rotary_fp16(X.data_ptr(), T, H, D, ldx, ldh, positions.data_ptr(), turns.data_ptr(), 2 * turns.numel(),
-                              1 if half else 0, magnitude, Y.data_ptr(), ldy, ldyh, _here(stream))
+                              1 if half else 0, magnitude, Y.data_ptr(), ldy, ldyh, _here(stream, X, positions, turns, Y))
     if code:
         _check(code)
 
@@ -591,7 +598,8 @@ def sq_cache_append(K, V, row_start, cached, table, page, cache, stream=None) ->
         raise ValueError("K and V must have the same shape")
     B, per_sequence, pages = _cache_args(Hk, D, row_start, cached, table, page, cache)
     code = lib.sq_cache_append(K.data_ptr(), ldk, V.data_ptr(), ldv, T, Hk, D, row_start.data_ptr(), cached.data_ptr(), B,
-                               table.data_ptr(), per_sequence, page, cache.data_ptr(), pages, _here(stream))
+                               table.data_ptr(), per_sequence, page, cache.data_ptr(), pages,
+                               _here(stream, K, V, row_start, cached, table, cache))
     if code:
         _check(code)
 
@@ -605,7 +613,8 @@ def sq_cache_read(cache, row_start, cached, table, page, K, V, stream=None) -> N
         raise ValueError("K and V must have the same shape")
     B, per_sequence, pages = _cache_args(Hk, D, row_start, cached, table, page, cache)
     code = lib.sq_cache_read(cache.data_ptr(), pages, Hk, D, row_start.data_ptr(), cached.data_ptr(), B, table.data_ptr(),
-                             per_sequence, page, K.data_ptr(), ldk, V.data_ptr(), ldv, T, _here(stream))
+                             per_sequence, page, K.data_ptr(), ldk, V.data_ptr(), ldv, T,
+                             _here(stream, K, V, row_start, cached, table, cache))
     if code:
         _check(code)
 
@@ -636,7 +645,8 @@ def sq_tree_attention(Q, row_start, cached, mask, table, page, cache, Hk, scale,
     code = lib.sq_tree_attention(
         Q.data_ptr(), ldq, T, Hq, Hk, D, row_start.data_ptr(), cached.data_ptr(), B, None if mask is None else mask.data_ptr(),
         max_rows, per_sequence * page if max_keys is None else max_keys, table.data_ptr(), per_sequence, page, cache.data_ptr(),
-        pages, scale, O.data_ptr(), ldo, ws, ws_bytes, _here(stream))
+        pages, scale, O.data_ptr(), ldo, ws, ws_bytes,
+        _here(stream, Q, row_start, cached, table, cache, O, Q if mask is None else mask, Q if workspace is None else workspace))
     if code:
         _check(code)
 

@@ -672,3 +672,16 @@ def test_product_of_many_channels(T, K, N, group):
     X, (codes, steps) = rows(g, T, K), weights(g, N, K, group)
     want, bound = ou.product(X, codes, steps, group, T > 32)
     ou.held(run_product(X, codes, steps, 8, 3), want, bound, f"{T} {K} {N} {group}")
+
+
+def test_a_table_left_on_the_host_is_refused():
+    import torch
+    import paper_2511_22316_amd as sq
+    x = torch.zeros(2, 3, 64, dtype=torch.float16, device="cuda")
+    positions = torch.zeros(2, dtype=torch.int32, device="cuda")
+    with pytest.raises(ValueError, match="device"):
+        sq.sq_rotary_fp16(x, positions, sq.sq_rotary_table(32), True, x)
+    sq.sq_rotary_fp16(x, positions, sq.sq_rotary_table(32).cuda(), True, x)
+    with pytest.raises(ValueError, match="device"):
+        sq.sq_quantize_grouped(x[0], 32, torch.zeros(3, 32, dtype=torch.uint8), torch.zeros(3, 2, dtype=torch.float16))
+    torch.cuda.synchronize()

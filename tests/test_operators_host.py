@@ -174,3 +174,20 @@ def test_bindings_refuse_wrong_types_and_shapes(lib):
         sq.sq_tree_attention(x, i(3), i(2), torch.zeros(2, dtype=torch.int32), i(2, 2), 16, cache, 3, 0.1, x.clone())
     with pytest.raises(ValueError):
         sq.sq_tree_attention(x, i(3), i(2), torch.zeros(1, dtype=torch.int64), i(2, 2), 16, cache, 3, 0.1, x.clone())
+
+
+def test_host_tensors_are_refused(lib):
+    """A kernel that follows a host pointer would take the process down."""
+    import torch
+    h = lambda *n: torch.zeros(n, dtype=torch.float16)      # noqa: E731
+    u = lambda *n: torch.zeros(n, dtype=torch.uint8)        # noqa: E731
+    i = lambda *n: torch.zeros(n, dtype=torch.int32)        # noqa: E731
+    x, cache = h(2, 3, 64), u(4 * sq.sq_cache_page_bytes(3, 64, 16))
+    for call in (lambda: sq.sq_quantize_grouped(h(2, 64), 32, u(2, 32), h(2, 2)),
+                 lambda: sq.sq_w4a16_gemm_grouped(h(2, 64), u(5, 32), h(5, 2), h(2, 5)),
+                 lambda: sq.sq_rotary_fp16(x, i(2), sq.sq_rotary_table(32), True, x),
+                 lambda: sq.sq_cache_append(x, x, i(3), i(2), i(2, 2), 16, cache),
+                 lambda: sq.sq_cache_read(cache, i(3), i(2), i(2, 2), 16, x, x),
+                 lambda: sq.sq_tree_attention(x, i(3), i(2), None, i(2, 2), 16, cache, 3, 0.1, x.clone())):
+        with pytest.raises(ValueError, match="device"):
+            call()
