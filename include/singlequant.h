@@ -420,7 +420,8 @@ sq_status sq_prepare_weights_variant(const void *W, int32_t K, int32_t N, int64_
  *   code[t, k] = clamp( floor(X[t, k] / step[t, g] + 1/2), -8, 7 )
  *
  * For weights: transpose, rotate (sq_rotate_fp16 on the rows of W^T), then this
- * call gives the operands of sq_w4a16_gemm_grouped.
+ * call gives the operands of sq_w4a16_gemm_grouped.  A group that holds an infinity
+ * or NaN gets a step that is not finite and codes that say nothing.
  *   X        device, fp16 [T, ldx]; rows 16-byte aligned (ldx % 8 == 0), ldx >= K
  *   group    32, 64, 128 or 256; K % group == 0, K <= 131072
  *   Q        device out, uint8 [T, K/2], 16-byte aligned; nibbles as everywhere
@@ -508,7 +509,9 @@ sq_status sq_rotary_fp16(const void *X, int64_t T, int32_t H, int32_t D, int64_t
  * sq_cache_append / sq_cache_read / sq_tree_attention -- keys and values in 4 bits.
  *
  * A row of K or V is Hk heads of D channels; every head is quantized for itself as a
- * group of sq_quantize_grouped is (codes in [-8, 7], one fp16 step).  The cache is
+ * group of sq_quantize_grouped is (codes in [-8, 7], one fp16 step), but for steps
+ * that would not be finite, which are 65504: an infinity is kept as the largest
+ * multiple of it, NaN as any, and a row that is not seen has no effect.  The cache is
  * `pages` pages of `page` rows, one buffer per layer, owned by the caller;
  * sq_cache_page_bytes is the size of a page (a multiple of 256; 0 for sizes that are
  * not covered).  Layout of a page, nibbles holding code + 8, the even channel low:
@@ -524,7 +527,8 @@ sq_status sq_rotary_fp16(const void *X, int64_t T, int32_t H, int32_t D, int64_t
  *   page       a power of two, 16 .. 1024; pages >= 0
  *   B          0 .. SQ_CACHE_MAX_SEQUENCES
  *   row_start  device, int32 [B + 1], not decreasing
- *   cached     device, int32 [B]
+ *   cached     device, int32 [B]; below zero: a sequence without keys, whose rows are
+ *              left out
  *   table      device, int32 [B, per_sequence]; page * per_sequence < 2^31
  *   cache      device, pages * sq_cache_page_bytes bytes, 16-byte aligned
  * The device arrays are read by the kernels only, so a captured graph goes with
@@ -570,7 +574,7 @@ sq_status sq_cache_read(const void *cache, int32_t pages, int32_t Hk, int32_t D,
  *              out: their rows of O keep what they held); <= 64 with a mask
  *   max_keys   about the longest cached[b] + new rows: how finely the work is split.
  *              Any value gives the right result.
- *   scale      in (0, 1e20); scores scale * Q . k beyond 2^26 are not told apart
+ *   scale      in (0, 1e20); scores scale * Q . k beyond 2^24 are not told apart
  *   workspace  device, 16-byte aligned, workspace_bytes long, or NULL and 0.  The sums
  *              of a split sequence meet in it; with less than
  *              sq_tree_attention_workspace_bytes the work is split less.  Nothing in

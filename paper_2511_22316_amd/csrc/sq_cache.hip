@@ -67,7 +67,8 @@ __global__ __launch_bounds__(256) void cache_append_kernel(const CacheView c, co
 #pragma unroll
         for (int k = 0; k < AT_ONCE; ++k) {
             const int unit = u0 + k * SHARE + lane;
-            const __half s = run_step(run_max<LANES>(x[k]));
+            // no step is infinite or NaN (either has more bits than 65504): the weight 0 of a row that is not seen gives 0
+            const __half s = __ushort_as_half(min(__half_as_ushort(run_step(run_max<LANES>(x[k]))), (unsigned short)0x7BFF));
             const uint32_t codes = run_codes_plus8(x[k], __builtin_amdgcn_rcpf(__half2float(s)));
             if (unit >= units) continue;
             const int head = unit / LANES, piece = unit % LANES;

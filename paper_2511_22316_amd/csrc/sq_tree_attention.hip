@@ -12,7 +12,7 @@ constexpr int kKeysPerTile = 32;       // of one wave and step
 constexpr int kWaves = 4;
 constexpr int kChunkUnit = kKeysPerTile * kWaves;
 constexpr int kMaxSplits = 64;         // a lane each in the kernel that joins them
-constexpr float kNothing = -1e30f;     // running maximum of a row that has seen no key
+constexpr float kNothing = -3e38f;     // running maximum of a row that has seen no key
 
 // Four fp16 of one dword pair.
 typedef _Float16 v4hs __attribute__((ext_vector_type(4)));
@@ -175,10 +175,11 @@ __global__ __launch_bounds__(kWaves *kWave, D == 256 || R == 2 ? 2 : 4) void tre
     if (row0 >= rows) return;
     const int page = 1 << c.page_shift;
     const uint32_t cap = (uint32_t)c.per_sequence << c.page_shift;
-    const uint32_t past = min((uint32_t)max(c.cached[b], 0), cap);
+    const int cached = c.cached[b];                // below zero: a sequence without keys
+    const uint32_t past = min((uint32_t)max(cached, 0), cap);
     // keys that the rows of this workgroup see at all, and that all of them see
     const int last_row = min(n, (row0 + 16 * R - 1) / a.group + 1);
-    const uint32_t limit = min(past + (uint32_t)(a.mask ? min(n, 64) : last_row), cap);
+    const uint32_t limit = cached < 0 ? 0u : min(past + (uint32_t)(a.mask ? min(n, 64) : last_row), cap);
     const uint32_t all_see = a.mask ? past : min(past + (uint32_t)(row0 / a.group) + 1, limit);
 
     const uint32_t half_codes = (uint32_t)page * (D / 2), head_at = (uint32_t)h * 2 * half_codes;
@@ -349,8 +350,9 @@ __global__ __launch_bounds__(kWaves *kWave, D == 256 || R == 2 ? 2 : 4) void tre
                     top = fmaxf(top, __builtin_fmaf(s[r][e / 4][e % 4], a.score_scale, log));
                 }
                 top = quarter_max(top);
-                // up by what the roundings of `top` and of the exponents may be off, which counts where scores are huge only
-                top = __builtin_fmaf(fabsf(top), 0x1p-22f, top);
+                // Where scores are huge their roundings count: M stays below the largest exponent by more than they are, so that
+                // key never vanishes, and products are held at 2^14.
+                top = __builtin_fmaf(fabsf(top), -0x1p-22f, top);
                 const float M_new = fmaxf(M[r], top - 7.9f), fade = __builtin_amdgcn_exp2f(M[r] - M_new);
                 M[r] = M_new;
                 l[r] *= fade;
@@ -358,6 +360,11 @@ __global__ __launch_bounds__(kWaves *kWave, D == 256 || R == 2 ? 2 : 4) void tre
 #pragma unroll
                 for (int j = 0; j < VT; ++j) o[r][j] *= fade;
                 weigh(r);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    w[r][e] = fminf(w[r][e], 0x1p14f * __builtin_amdgcn_rcpf(step_v[e]));
+                    product[r][e] = w[r][e] * step_v[e];
+                }
             }
         }
         v8h p[R];

@@ -194,8 +194,10 @@ __global__ __launch_bounds__(NW *kWave) void w4a16_grouped_skinny_kernel(const _
 // The steps of a round are one load: every quarter of a wave takes a quarter of them, and swaps hand them to the others.
 // (A step load per slice touches 16 cache lines for two bytes of each, which the codes have pushed out of the CU's cache
 // again by the next slice: 43 us at T = 8, K = 8192, N = 28672, groups of 128; all steps of a round in every quarter
-// 33.5, and 46 with groups of 32.)  Where K is no whole number of rounds the last slice is taken again with steps of zero.
+// 33.5, and 46 with groups of 32.)  Where K is no whole number of rounds the rows go on with zeros, and the last slice of codes is taken
+// again with them and with steps of zero.
 constexpr int kRowPad = 16;            // bytes; sixteen rows then start in sixteen different 16-byte bank groups
+inline __host__ __device__ int row_bytes(int K, int per_round) { return 2 * ((K + per_round - 1) / per_round * per_round) + kRowPad; }
 
 // A dword of every quarter of the wave, in all of them.
 __device__ __forceinline__ void all_quarters(uint32_t v, uint32_t (&of)[4])
@@ -224,7 +226,7 @@ __global__ __launch_bounds__(NW *kWave) void w4a16_grouped_rows_kernel(const __h
     char *xs = reinterpret_cast<char *>(rows_u4);
     const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(tid / kWave);
     const int l16 = lane & 15, q = lane >> 4;
-    const int stride = 2 * K + kRowPad, slices = K / 128, groups = K / GROUP, rounds = (slices + NR - 1) / NR;
+    const int stride = row_bytes(K, NR * 128), slices = K / 128, groups = K / GROUP, rounds = (slices + NR - 1) / NR;
     const int blocks = (N + 15) / 16, mine = (blocks - (int)blockIdx.x + (int)gridDim.x - 1) / (int)gridDim.x;
     // this wave's run: rounds [begin, end) of the workgroup's mine * rounds, numbered block after block
     const int64_t all = (int64_t)mine * rounds;
@@ -295,6 +297,9 @@ __global__ __launch_bounds__(NW *kWave) void w4a16_grouped_rows_kernel(const __h
                 *reinterpret_cast<uint4 *>(xs + (j / chunks_per_row) * stride + 16 * (j % chunks_per_row)) = interleave_halves(xv[u]);
         }
     }
+    const int tail = rounds * NR * 16 - chunks_per_row;                        // chunks of zeros behind a row
+    for (int j = tid; j < T * tail; j += NT)
+        *reinterpret_cast<uint4 *>(xs + (j / tail) * stride + 16 * (chunks_per_row + j % tail)) = uint4{0u, 0u, 0u, 0u};
     __syncthreads();
 
     uint32_t magic;                                    // 1024.0 in both halves, held in a vector register
@@ -326,7 +331,7 @@ __global__ __launch_bounds__(NW *kWave) void w4a16_grouped_rows_kernel(const __h
         ask_steps();
 #pragma unroll
         for (int k = 0; k < NR; ++k) {
-            read_tokens((k + 1) & 1, k + 1 == NR ? next * NR : min(round * NR + k + 1, slices - 1));
+            read_tokens((k + 1) & 1, k + 1 == NR ? next * NR : round * NR + k + 1);
             uint32_t d[4] = {w[k].x, w[k].y, w[k].z, w[k].w};
             sort_steps<GROUP>(d);
 #pragma unroll
@@ -401,7 +406,7 @@ sq_status launch_grouped_rows(const GroupedArgs &a)
     const int blocks = (a.N + 15) / 16, grid = blocks < 256 ? blocks : 256;
     auto kernel = w4a16_grouped_rows_kernel<GROUP, NW, NR>;
     if (!allow_large_lds(reinterpret_cast<const void *>(kernel))) return SQ_ERR_LAUNCH;
-    const size_t rows = (size_t)a.T * (2 * a.K + kRowPad), heads = (size_t)NW * kWave * 16;
+    const size_t rows = (size_t)a.T * row_bytes(a.K, NR * 128), heads = (size_t)NW * kWave * 16;
     hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(NW * kWave), rows > heads ? rows : heads, a.st, a.X, a.ldx, a.T, a.K, a.Qw, a.steps, a.N,
                        a.Y, a.ldy);
     return hipGetLastError() == hipSuccess ? SQ_OK : SQ_ERR_LAUNCH;
@@ -414,7 +419,7 @@ sq_status launch_grouped_few(const GroupedArgs &a)
     // Token rows in LDS where they fit and there is enough to share out evenly (us, that / the other kernel at its best, T = 1,
     // groups of 128: K = 4096, N = 8192 9.0 / 7.7, N = 9216 10.3 / 12.0; K = 8192, N = 8192 12.7 / 13.7, N = 28672 28.9 / 38.0), at
     // more than one block of channels per workgroup (K = 11008, N = 4096 10.9 / 10.1).
-    if (tiles == 1 && a.K % 128 == 0 && a.T * (int64_t)(2 * a.K + kRowPad) <= kMaxDynamicLds && blocks > 256 && (int64_t)a.K * a.N > ((int64_t)32 << 20))
+    if (tiles == 1 && a.K % 128 == 0 && (int64_t)a.T * row_bytes(a.K, 512) <= kMaxDynamicLds && blocks > 256 && (int64_t)a.K * a.N > ((int64_t)32 << 20))
         return launch_grouped_rows<GROUP, 8, 4>(a);
     // The fewest channels per workgroup that need one round of workgroups on the 256 CUs (us with 16 / 32 / 64 channels, T = 1,
     // K = 4096, groups of 128: N = 4096 5.8 / 7.4 / 11.8, N = 6144 9.0 / 7.5 / 12.0, N = 9216 12.2 / 12.7 / 12.0), and both blocks of

@@ -685,3 +685,85 @@ def test_a_table_left_on_the_host_is_refused():
     with pytest.raises(ValueError, match="device"):
         sq.sq_quantize_grouped(x[0], 32, torch.zeros(3, 32, dtype=torch.uint8), torch.zeros(3, 2, dtype=torch.float16))
     torch.cuda.synchronize()
+
+
+def test_product_keeps_an_infinity_where_it_is():
+    """A token with an infinity: infinite (or NaN where a code is 0) in its own row, and nothing of it in the others; rows in LDS with
+    a K that is no whole number of rounds among them."""
+    print("case product infinity", flush=True)
+    for T, K, N, group in ((5, 4736, 7200, 128), (5, 4736, 7200, 32), (3, 320, 40, 64), (40, 384, 300, 32)):
+        g = rng(15, T, K, N, group)
+        X, (codes, steps) = rows(g, T, K), weights(g, N, K, group)
+        codes[:, K - 1] = 2 * (codes[:, K - 1] >= 0) - 1    # the place of the infinity: never 0
+        want, bound = ou.product(X, codes, steps, group, T > 32)
+        X[1, K - 1] = np.inf
+        got = run_product(X, codes, steps)
+        assert (got[1].astype(np.float64) == np.inf * codes[:, K - 1]).all(), (T, K, N, group)
+        others = np.arange(T) != 1
+        ou.held(got[others], want[others], bound[others], "others")
+
+
+def test_attention_rows_that_do_not_see_an_infinity():
+    """Keys and values that are not finite, in rows that a mask hides."""
+    import paper_2511_22316_amd as sq
+    print("case attention hidden infinity", flush=True)
+    for D in (64, 128, 256):
+        s = Setting(1000 + D, [40, 0], [20, 9], 2, D, 16)
+        Q = s.queries(8)
+        words = s.trees()
+        bad = np.uint64(1) << np.uint64(3)                  # new row 3 of both sequences
+        seeing = (words & bad) != 0
+        assert seeing.any() and not seeing.all()
+        kv = np.full((2, 2, D), np.inf, np.float16)
+        kv[:, :, 1::2] = np.nan
+        slots = dev(np.array([0, 1, 2], np.int32)), dev((s.past + 3).astype(np.int32)), s.dtable
+        sq.sq_cache_append(dev(kv), dev(kv), *slots, 16, s.cache)
+        want, bound = s.expect(Q, 4, s.by_mask(words & ~bad), 0.2)
+        for max_keys in (None, MANY_KEYS):
+            got = s.run(Q, words, 0.2, max_keys=max_keys)
+            ou.held(got[~seeing], want[~seeing], bound[~seeing], f"hidden {D}")
+
+
+def test_attention_scores_of_one_sign_far_from_zero():
+    """A score near -10^27 or +10^27 with no other beside it: the value, not zeros."""
+    print("case attention scores far below zero", flush=True)
+    for sign in (-1, 1):
+        one = Setting(80, [0], [1], 1, 64, 16)
+        key, value = one.numbers.values(0, 0, 1)[0][0, 0], one.numbers.values(0, 1, 1)[0][0, 0]
+        Q = np.broadcast_to((sign * np.sign(key) * 60000).astype(np.float16), (1, 2, 64))
+        got = one.run(np.ascontiguousarray(Q), None, 9e19)
+        # the weight and the result are rounded to fp16; the eights come off sums of 16 steps
+        step = np.abs(value).max() / 7
+        bound = (2 * ou.HALF + ou.HALF ** 2 + 8 * ou.EPS32) * np.abs(value) + 40 * ou.EPS32 * 16 * step + ou.TINY
+        ou.held(got[0], np.broadcast_to(value, (2, 64)), np.broadcast_to(bound, (2, 64)), f"{sign}")
+
+
+def test_attention_of_a_sequence_with_a_negative_length():
+    print("case attention negative length", flush=True)
+    s = Setting(81, [20, 30], [2, 3], 2, 64, 16)
+    Q = s.queries(4)
+    want, bound = s.expect(Q, 2, s.causal, 0.2)
+    s.dcached = dev(np.array([20, -1], np.int32))
+    got = s.run(Q, None, 0.2)
+    ou.held(got[:2], want[:2], bound[:2], "the other sequence")
+    assert (got[2:] == 0).all()
+
+
+def test_cache_keeps_infinities_as_large_numbers():
+    import torch
+    import paper_2511_22316_amd as sq
+    print("case cache infinity", flush=True)
+    x = np.ones((3, 2, 128), np.float16)
+    x[0, 0, 5], x[1, 1, 7], x[2, 0, 9] = np.inf, -np.inf, np.nan
+    cache = torch.zeros(1, sq.sq_cache_page_bytes(2, 128, 16), dtype=torch.uint8, device="cuda")
+    args = dev(np.array([0, 3], np.int32)), dev(np.zeros(1, np.int32)), dev(np.zeros((1, 1), np.int32)), 16
+    sq.sq_cache_append(dev(x), dev(x), *args, cache)
+    k, v = (torch.empty(3, 2, 128, dtype=torch.float16, device="cuda") for _ in range(2))
+    sq.sq_cache_read(cache, *args, k, v)
+    k, v = host(k), host(v)
+    assert np.array_equal(k[0, 0], np.where(np.arange(128) == 5, np.inf, 0.0)) and np.array_equal(v[0, 0], k[0, 0])
+    assert np.array_equal(k[1, 1], np.where(np.arange(128) == 7, -np.inf, 0.0)) and np.array_equal(v[1, 1], k[1, 1])
+    other = np.arange(128) != 9
+    assert (k[2, 0][other] == 0).all() and (k[0, 1] == k[2, 1]).all() and abs(float(k[0, 1, 0]) - 1) < 0.01
+    steps = host(cache).view(np.float16)[0, (2 * 16 * 128) // 2: (2 * 16 * 132) // 2]
+    assert np.isfinite(steps).all()
