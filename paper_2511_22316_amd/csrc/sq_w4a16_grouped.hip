@@ -379,6 +379,163 @@ __global__ __launch_bounds__(NW *kWave) void w4a16_grouped_rows_kernel(const __h
     store(block, total);
 }
 
+// ---- at most 32 tokens whose rows do not fit in LDS -----------------------------------------------
+// The rows pass through LDS in parts of 1024 channels, two of them there at a time: the next one goes to registers at a
+// part's start and from there to LDS at its end.  A workgroup owns NW blocks of 16 channels over all of K; KG waves share a
+// block, each with its slices of every part, and add up at the end.  A wave requests a slice of the next part when it is done
+// with the same slice of this one.  Steps, and the turn by which workgroups begin with another part, as above.
+// What a wave does for a slice is a chain (LDS, matrix instructions, scaling), so four waves per SIMD are better than two where
+// the steps are many (us, T = 32, K = 8192, N = 28672, groups of 128 / 64 / 32: 38 / 49.5 / 59 with two, 36.4 / 40.8 / 49.8 so;
+// the kernel for few tokens 66 / 74 / 73).
+constexpr int kPart = 1024, kPartRow = 2 * kPart + kRowPad;
+
+template <int GROUP, int TT, int NW, int KG>
+__global__ __launch_bounds__(NW *KG *kWave) void w4a16_grouped_parts_kernel(const __half *__restrict__ X, int64_t ldx, int T, int K,
+                                                                        const uint8_t *__restrict__ Qw, const __half *__restrict__ steps,
+                                                                        int N, __half *__restrict__ Y, int64_t ldy)
+{
+    constexpr int NT = NW * KG * kWave, NR = kPart / 128 / KG, SUB = GROUP >= 128 ? 1 : 128 / GROUP, CHAIN = 4 / SUB;
+    // codes and steps of a wave's share of a part (which may be half a group), steps of a quarter of the wave
+    constexpr int SPAN = NR * 128, SPR = SPAN < GROUP ? 1 : SPAN / GROUP, PIECE = SPR < 4 ? 1 : SPR / 4;
+    constexpr int SETS = TT * KG > 2 ? 1 : 2;                                  // of token chunks: what the registers hold
+    constexpr int CHUNKS = 16 * TT * (kPart / 8) / NT;                         // 16-byte chunks of a part of the rows per thread
+    struct __attribute__((packed, aligned(2))) Piece {
+        unsigned short s[PIECE];
+    };
+    extern __shared__ uint4 rows_u4[];
+    char *xs = reinterpret_cast<char *>(rows_u4);
+    const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(tid / kWave);
+    const int l16 = lane & 15, q = lane >> 4;
+    const int slices = K / 128, groups = K / GROUP, parts = (K + kPart - 1) / kPart;
+    const int kg = wave / NW, n0 = 16 * ((int)blockIdx.x * NW + wave % NW);
+    const int64_t channel = min(n0 + l16, N - 1);
+    const uint8_t *w_row = Qw + channel * (K / 2) + 16 * q;
+    const __half *s_row = steps + channel * groups;
+    const int turn = (int)blockIdx.x % parts;
+    auto part_at = [&](int p) {                        // the p-th part in this workgroup's order; behind the last its first again
+        const int at = p + turn;
+        return at >= parts ? at - parts : at;
+    };
+
+    uint4 xv[CHUNKS], w[NR];
+    Piece s;
+    auto ask_tokens = [&](int part) {
+#pragma unroll
+        for (int u = 0; u < CHUNKS; ++u) {
+            const int j = tid + NT * u, row = j / (kPart / 8), k = part * kPart + 8 * (j % (kPart / 8));
+            xv[u] = *reinterpret_cast<const uint4 *>(X + (int64_t)min(row, T - 1) * ldx + min(k, K - 8));
+        }
+    };
+    auto put_tokens = [&](int part, int buffer) {      // zeros behind the row's end
+#pragma unroll
+        for (int u = 0; u < CHUNKS; ++u) {
+            const int j = tid + NT * u, row = j / (kPart / 8), c = j % (kPart / 8);
+            const uint4 v = interleave_halves(xv[u]);
+            const bool in = part * kPart + 8 * c < K;
+            *reinterpret_cast<uint4 *>(xs + (buffer * 16 * TT + row) * kPartRow + 16 * c) = uint4{in ? v.x : 0u, in ? v.y : 0u, in ? v.z : 0u, in ? v.w : 0u};
+        }
+    };
+    auto ask_codes = [&](int part, int k) { w[k] = *reinterpret_cast<const uint4 *>(w_row + min(NR * (part * KG + kg) + k, slices - 1) * 64); };
+    auto ask_steps = [&](int part) {
+        const int from = (part * KG + kg) * SPAN / GROUP, at = from + q * PIECE;
+        if (from + 4 * PIECE <= groups) {
+            s = *reinterpret_cast<const Piece *>(s_row + at);
+        } else {
+#pragma unroll
+            for (int g = 0; g < PIECE; ++g) {
+                const unsigned short v = __half_as_ushort(s_row[min(at + g, groups - 1)]);
+                s.s[g] = at + g < groups ? v : 0;
+            }
+        }
+    };
+    ask_tokens(part_at(0));
+    ask_steps(part_at(0));
+#pragma unroll
+    for (int k = 0; k < NR; ++k) ask_codes(part_at(0), k);
+    put_tokens(part_at(0), 0);
+    __syncthreads();
+
+    uint32_t magic;                                    // 1024.0 in both halves, held in a vector register
+    asm volatile("v_mov_b32 %0, 0x64006400" : "=v"(magic));
+    v4f total[TT];
+#pragma unroll
+    for (int i = 0; i < TT; ++i) total[i] = v4f{0.f, 0.f, 0.f, 0.f};
+    for (int p = 0; p < parts; ++p) {
+        const int next = part_at(p + 1 < parts ? p + 1 : p);
+        ask_tokens(next);
+        uint32_t now[(PIECE + 1) / 2][4];                             // the steps of this part, two to a dword
+#pragma unroll
+        for (int g = 0; g < PIECE; g += 2) all_quarters(s.s[g] | (g + 1 < PIECE ? (uint32_t)s.s[g + 1 < PIECE ? g + 1 : g] << 16 : 0u), now[g / 2]);
+        ask_steps(next);
+        const char *xa = xs + ((p & 1) * 16 * TT + l16) * kPartRow;
+        v8h x[SETS][TT][4];
+        auto read_tokens = [&](int set, int k) {
+#pragma unroll
+            for (int i = 0; i < TT; ++i)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) x[set][i][j] = *reinterpret_cast<const v8h *>(xa + i * (16 * kPartRow) + 256 * (kg * NR + k) + 2 * slice_place<GROUP>(j, q));
+        };
+        if constexpr (SETS == 2) read_tokens(0, 0);
+#pragma unroll
+        for (int k = 0; k < NR; ++k) {
+            if constexpr (SETS == 1)
+                read_tokens(0, k);
+            else if (k + 1 < NR)
+                read_tokens((k + 1) & 1, k + 1);
+            uint32_t d[4] = {w[k].x, w[k].y, w[k].z, w[k].w};
+            sort_steps<GROUP>(d);
+#pragma unroll
+            for (int g = 0; g < SUB; ++g) {
+                v4f part[TT];
+#pragma unroll
+                for (int j = g * CHAIN; j < (g + 1) * CHAIN; ++j) {
+                    const v8h b = widen_codes_f16(d[j], magic);
+#pragma unroll
+                    for (int i = 0; i < TT; ++i)
+                        part[i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(x[k % SETS][i][j], b, j == g * CHAIN ? v4f{0.f, 0.f, 0.f, 0.f} : part[i], 0, 0, 0);
+                }
+                const int step = k * SPR / NR + g, in = step % PIECE;          // of the part, of the quarter
+                const uint32_t pair = now[in / 2][step / PIECE];
+                const float f = __half2float(__ushort_as_half((unsigned short)(in % 2 ? pair >> 16 : pair)));
+#pragma unroll
+                for (int i = 0; i < TT; ++i)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) total[i][e] = __builtin_fmaf(f, part[i][e], total[i][e]);
+            }
+            ask_codes(next, k);
+            // as above: the requests stay here, one slice behind another
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        put_tokens(next, (p + 1) & 1);
+        __syncthreads();
+    }
+    if constexpr (KG > 1) {
+        v4f *sums = reinterpret_cast<v4f *>(rows_u4);
+        if (kg > 0)
+#pragma unroll
+            for (int i = 0; i < TT; ++i) sums[((wave - NW) * TT + i) * kWave + lane] = total[i];
+        __syncthreads();
+        if (kg > 0) return;
+#pragma unroll
+        for (int v = 1; v < KG; ++v)
+#pragma unroll
+            for (int i = 0; i < TT; ++i) {
+                const v4f more = sums[((wave + (v - 1) * NW) * TT + i) * kWave + lane];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) total[i][e] += more[e];
+            }
+    }
+    // 16 x 16 accumulator layout: lane holds channel l16, register e holds token 4 q + e
+    const int n = n0 + l16;
+#pragma unroll
+    for (int i = 0; i < TT; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const int t = 16 * i + 4 * q + e;
+            if (t < T && n < N) Y[(int64_t)t * ldy + n] = __float2half_rn(total[i][e]);
+        }
+}
+
 struct GroupedArgs {
     const __half *X;
     int64_t ldx;
@@ -412,15 +569,36 @@ sq_status launch_grouped_rows(const GroupedArgs &a)
     return hipGetLastError() == hipSuccess ? SQ_OK : SQ_ERR_LAUNCH;
 }
 
+template <int GROUP, int TT, int NW, int KG>
+sq_status launch_grouped_parts(const GroupedArgs &a)
+{
+    auto kernel = w4a16_grouped_parts_kernel<GROUP, TT, NW, KG>;
+    if (!allow_large_lds(reinterpret_cast<const void *>(kernel))) return SQ_ERR_LAUNCH;
+    const int64_t blocks = ((int64_t)a.N + 15) / 16;
+    hipLaunchKernelGGL(kernel, dim3((unsigned)((blocks + NW - 1) / NW)), dim3(NW * KG * kWave), 2 * 16 * TT * kPartRow, a.st, a.X, a.ldx, a.T, a.K, a.Qw,
+                       a.steps, a.N, a.Y, a.ldy);
+    return hipGetLastError() == hipSuccess ? SQ_OK : SQ_ERR_LAUNCH;
+}
+
 template <int GROUP>
 sq_status launch_grouped_few(const GroupedArgs &a)
 {
     const int64_t tiles = (a.T + 15) / 16, blocks = (a.N + 15) / 16;
-    // Token rows in LDS where they fit and there is enough to share out evenly (us, that / the other kernel at its best, T = 1,
-    // groups of 128: K = 4096, N = 8192 9.0 / 7.7, N = 9216 10.3 / 12.0; K = 8192, N = 8192 12.7 / 13.7, N = 28672 28.9 / 38.0), at
-    // more than one block of channels per workgroup (K = 11008, N = 4096 10.9 / 10.1).
-    if (tiles == 1 && a.K % 128 == 0 && (int64_t)a.T * row_bytes(a.K, 512) <= kMaxDynamicLds && blocks > 256 && (int64_t)a.K * a.N > ((int64_t)32 << 20))
-        return launch_grouped_rows<GROUP, 8, 4>(a);
+    const bool slices = a.K % 128 == 0, large = (int64_t)a.K * a.N > ((int64_t)32 << 20) && blocks > 256;
+    // Token rows in LDS where they fit and there is enough to share out evenly (us, that / the kernel for few tokens at its best,
+    // T = 1, groups of 128: K = 4096, N = 8192 9.0 / 7.7, N = 9216 10.3 / 12.0; K = 8192, N = 8192 12.7 / 13.7, N = 28672 28.9 / 38.0),
+    // at more than one block of channels per workgroup (K = 11008, N = 4096 10.9 / 10.1).
+    if (tiles == 1 && slices && large && (int64_t)a.T * row_bytes(a.K, 512) <= kMaxDynamicLds) return launch_grouped_rows<GROUP, 8, 4>(a);
+    // In parts where they do not fit, or are more than 16 over a K worth the two barriers of a part (us, parts / the kernel for few
+    // tokens, groups of 128: T = 16, K = 8192, N = 28672 31.0 / 47.8, K = 5120, N = 13824 14.6 / 17.5, K = 8192, N = 8192 16.2 / 18.2, but
+    // T = 8, K = 28672, N = 8192 42.1 / 39.3; T = 32, K = 1024, N = 28672 9.1 / 12.4, N = 16384 7.4 / 7.2; K = 2048, N = 16384 9.9 / 11.6;
+    // K = 4096, N = 8192 11.9 / 13.9).  Channels per workgroup: one round of workgroups again; groups of 32 and 64 want the waves.
+    if (slices && blocks > 256 && (tiles == 2 ? a.K >= (blocks > 1024 ? 1024 : 2048) : large && (a.T > 8 || blocks > 512))) {
+        constexpr int KG = GROUP <= 64 ? 4 : 2;
+        if (blocks > 1024) return tiles == 2 ? launch_grouped_parts<GROUP, 2, 8, 2>(a) : launch_grouped_parts<GROUP, 1, 8, 2>(a);
+        if (blocks > 512) return tiles == 2 ? launch_grouped_parts<GROUP, 2, 4, KG>(a) : launch_grouped_parts<GROUP, 1, 4, KG>(a);
+        return tiles == 2 ? launch_grouped_parts<GROUP, 2, 2, 8>(a) : launch_grouped_parts<GROUP, 1, 2, 8>(a);
+    }
     // The fewest channels per workgroup that need one round of workgroups on the 256 CUs (us with 16 / 32 / 64 channels, T = 1,
     // K = 4096, groups of 128: N = 4096 5.8 / 7.4 / 11.8, N = 6144 9.0 / 7.5 / 12.0, N = 9216 12.2 / 12.7 / 12.0), and both blocks of
     // 16 tokens in a workgroup before there are two rounds (T = 32, N = 11008 26.0 / 19.8).  Groups of 32 and 64 have more
@@ -470,8 +648,6 @@ extern "C" sq_status sq_w4a16_gemm_grouped(const void *X, int64_t T, int32_t K, 
         return SQ_ERR_ALIGN;
     const sq::GroupedArgs a = {static_cast<const __half *>(X), ldx, (int)T, K, Qw, static_cast<const __half *>(steps), group, N,
                                static_cast<__half *>(Y), ldy, static_cast<hipStream_t>(stream)};
-    // (From 17 tokens on the tiles would be the faster ones where the pass over the codes takes two rounds of workgroups, T = 32,
-    // K = 4096, N = 22016 28.4 us for 37.0, but they round every weight to fp16: up to 32 tokens keep theirs as they are.)
     if (T > 32) return sq::launch_grouped_many(a);
     if (group == 32) return sq::launch_grouped_few<32>(a);
     if (group == 64) return sq::launch_grouped_few<64>(a);

@@ -767,3 +767,20 @@ def test_cache_keeps_infinities_as_large_numbers():
     assert (k[2, 0][other] == 0).all() and (k[0, 1] == k[2, 1]).all() and abs(float(k[0, 1, 0]) - 1) < 0.01
     steps = host(cache).view(np.float16)[0, (2 * 16 * 128) // 2: (2 * 16 * 132) // 2]
     assert np.isfinite(steps).all()
+
+
+@pytest.mark.parametrize("T,K,N,group", [(32, 2048, 4200, 32), (17, 2304, 4100, 256), (25, 2176, 8300, 64), (31, 2048, 9000, 128), (24, 1024, 17000, 128),
+                                         (32, 1152, 16500, 32), (16, 5120, 16400, 64), (13, 6528, 8200, 128), (16, 5120, 9000, 32),
+                                         (12, 8192, 4300, 32), (16, 5376, 7000, 256)])
+def test_product_in_parts(T, K, N, group):
+    """Token rows that pass through LDS in parts."""
+    print(f"case product in parts {T} {K} {N} {group}", flush=True)
+    g = rng(16, T, K, N, group)
+    X, (codes, steps) = rows(g, T, K), weights(g, N, K, group)
+    codes[:, K - 1] = 2 * (codes[:, K - 1] >= 0) - 1
+    want, bound = ou.product(X, codes, steps, group)
+    ou.held(run_product(X, codes, steps, 8, 3), want, bound, f"{T} {K} {N} {group}")
+    X[T - 1, K - 1] = np.inf                                # stays in its row, also where the last part is not full
+    got = run_product(X, codes, steps)
+    assert (got[T - 1].astype(np.float64) == np.inf * codes[:, K - 1]).all()
+    ou.held(got[: T - 1], want[: T - 1], bound[: T - 1], "others")
