@@ -381,18 +381,19 @@ __global__ __launch_bounds__(NW *kWave) void w4a16_grouped_rows_kernel(const __h
 
 // ---- at most 32 tokens whose rows do not fit in LDS -----------------------------------------------
 // The rows pass through LDS in parts of 1024 channels, two of them there at a time: the next one goes to registers at a
-// part's start and from there to LDS at its end.  A workgroup owns NW blocks of 16 channels over all of K; KG waves share a
-// block, each with its slices of every part, and add up at the end.  A wave requests a slice of the next part when it is done
-// with the same slice of this one.  Steps, and the turn by which workgroups begin with another part, as above.
-// What a wave does for a slice is a chain (LDS, matrix instructions, scaling), so four waves per SIMD are better than two where
-// the steps are many (us, T = 32, K = 8192, N = 28672, groups of 128 / 64 / 32: 38 / 49.5 / 59 with two, 36.4 / 40.8 / 49.8 so;
-// the kernel for few tokens 66 / 74 / 73).
+// part's start and from there to LDS at its end.  A workgroup owns up to NW blocks of 16 channels over all of K, as many as
+// make whole rounds of workgroups (T = 32, K = 8192, N = 18000: 35.4 us with all eight in each, 29.2 so); KG waves share a block,
+// each with its slices of every part, and add up at the end.  A wave requests a slice of the next part when it is done with
+// the same slice of this one.  Steps, and the turn by which workgroups begin with another part, as above.
+// What a wave does for a slice is a chain (LDS, matrix instructions, scaling), so four waves per SIMD are better than two (us,
+// T = 32, K = 8192, N = 28672, groups of 128 / 64 / 32: KG = 1 37.2 / 41.0 / 45.7, KG = 2 35.5 / 38.6 / 42.4; the kernel for few tokens
+// 66 / 74 / 73).
 constexpr int kPart = 1024, kPartRow = 2 * kPart + kRowPad;
 
 template <int GROUP, int TT, int NW, int KG>
 __global__ __launch_bounds__(NW *KG *kWave) void w4a16_grouped_parts_kernel(const __half *__restrict__ X, int64_t ldx, int T, int K,
                                                                         const uint8_t *__restrict__ Qw, const __half *__restrict__ steps,
-                                                                        int N, __half *__restrict__ Y, int64_t ldy)
+                                                                        int N, __half *__restrict__ Y, int64_t ldy, int own)
 {
     constexpr int NT = NW * KG * kWave, NR = kPart / 128 / KG, SUB = GROUP >= 128 ? 1 : 128 / GROUP, CHAIN = 4 / SUB;
     // codes and steps of a wave's share of a part (which may be half a group), steps of a quarter of the wave
@@ -407,7 +408,8 @@ __global__ __launch_bounds__(NW *KG *kWave) void w4a16_grouped_parts_kernel(cons
     const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(tid / kWave);
     const int l16 = lane & 15, q = lane >> 4;
     const int slices = K / 128, groups = K / GROUP, parts = (K + kPart - 1) / kPart;
-    const int kg = wave / NW, n0 = 16 * ((int)blockIdx.x * NW + wave % NW);
+    const int kg = wave / NW, n0 = 16 * ((int)blockIdx.x * own + wave % NW);
+    const bool works = wave % NW < own;                // the others carry tokens only
     const int64_t channel = min(n0 + l16, N - 1);
     const uint8_t *w_row = Qw + channel * (K / 2) + 16 * q;
     const __half *s_row = steps + channel * groups;
@@ -449,9 +451,11 @@ __global__ __launch_bounds__(NW *KG *kWave) void w4a16_grouped_parts_kernel(cons
         }
     };
     ask_tokens(part_at(0));
-    ask_steps(part_at(0));
+    if (works) {
+        ask_steps(part_at(0));
 #pragma unroll
-    for (int k = 0; k < NR; ++k) ask_codes(part_at(0), k);
+        for (int k = 0; k < NR; ++k) ask_codes(part_at(0), k);
+    }
     put_tokens(part_at(0), 0);
     __syncthreads();
 
@@ -463,48 +467,50 @@ __global__ __launch_bounds__(NW *KG *kWave) void w4a16_grouped_parts_kernel(cons
     for (int p = 0; p < parts; ++p) {
         const int next = part_at(p + 1 < parts ? p + 1 : p);
         ask_tokens(next);
-        uint32_t now[(PIECE + 1) / 2][4];                             // the steps of this part, two to a dword
+        if (works) {
+            uint32_t now[(PIECE + 1) / 2][4];                             // the steps of this part, two to a dword
 #pragma unroll
-        for (int g = 0; g < PIECE; g += 2) all_quarters(s.s[g] | (g + 1 < PIECE ? (uint32_t)s.s[g + 1 < PIECE ? g + 1 : g] << 16 : 0u), now[g / 2]);
-        ask_steps(next);
-        const char *xa = xs + ((p & 1) * 16 * TT + l16) * kPartRow;
-        v8h x[SETS][TT][4];
-        auto read_tokens = [&](int set, int k) {
-#pragma unroll
-            for (int i = 0; i < TT; ++i)
-#pragma unroll
-                for (int j = 0; j < 4; ++j) x[set][i][j] = *reinterpret_cast<const v8h *>(xa + i * (16 * kPartRow) + 256 * (kg * NR + k) + 2 * slice_place<GROUP>(j, q));
-        };
-        if constexpr (SETS == 2) read_tokens(0, 0);
-#pragma unroll
-        for (int k = 0; k < NR; ++k) {
-            if constexpr (SETS == 1)
-                read_tokens(0, k);
-            else if (k + 1 < NR)
-                read_tokens((k + 1) & 1, k + 1);
-            uint32_t d[4] = {w[k].x, w[k].y, w[k].z, w[k].w};
-            sort_steps<GROUP>(d);
-#pragma unroll
-            for (int g = 0; g < SUB; ++g) {
-                v4f part[TT];
-#pragma unroll
-                for (int j = g * CHAIN; j < (g + 1) * CHAIN; ++j) {
-                    const v8h b = widen_codes_f16(d[j], magic);
-#pragma unroll
-                    for (int i = 0; i < TT; ++i)
-                        part[i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(x[k % SETS][i][j], b, j == g * CHAIN ? v4f{0.f, 0.f, 0.f, 0.f} : part[i], 0, 0, 0);
-                }
-                const int step = k * SPR / NR + g, in = step % PIECE;          // of the part, of the quarter
-                const uint32_t pair = now[in / 2][step / PIECE];
-                const float f = __half2float(__ushort_as_half((unsigned short)(in % 2 ? pair >> 16 : pair)));
+            for (int g = 0; g < PIECE; g += 2) all_quarters(s.s[g] | (g + 1 < PIECE ? (uint32_t)s.s[g + 1 < PIECE ? g + 1 : g] << 16 : 0u), now[g / 2]);
+            ask_steps(next);
+            const char *xa = xs + ((p & 1) * 16 * TT + l16) * kPartRow;
+            v8h x[SETS][TT][4];
+            auto read_tokens = [&](int set, int k) {
 #pragma unroll
                 for (int i = 0; i < TT; ++i)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) total[i][e] = __builtin_fmaf(f, part[i][e], total[i][e]);
+                    for (int j = 0; j < 4; ++j) x[set][i][j] = *reinterpret_cast<const v8h *>(xa + i * (16 * kPartRow) + 256 * (kg * NR + k) + 2 * slice_place<GROUP>(j, q));
+            };
+            if constexpr (SETS == 2) read_tokens(0, 0);
+#pragma unroll
+            for (int k = 0; k < NR; ++k) {
+                if constexpr (SETS == 1)
+                    read_tokens(0, k);
+                else if (k + 1 < NR)
+                    read_tokens((k + 1) & 1, k + 1);
+                uint32_t d[4] = {w[k].x, w[k].y, w[k].z, w[k].w};
+                sort_steps<GROUP>(d);
+#pragma unroll
+                for (int g = 0; g < SUB; ++g) {
+                    v4f part[TT];
+#pragma unroll
+                    for (int j = g * CHAIN; j < (g + 1) * CHAIN; ++j) {
+                        const v8h b = widen_codes_f16(d[j], magic);
+#pragma unroll
+                        for (int i = 0; i < TT; ++i)
+                            part[i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(x[k % SETS][i][j], b, j == g * CHAIN ? v4f{0.f, 0.f, 0.f, 0.f} : part[i], 0, 0, 0);
+                    }
+                    const int step = k * SPR / NR + g, in = step % PIECE;          // of the part, of the quarter
+                    const uint32_t pair = now[in / 2][step / PIECE];
+                    const float f = __half2float(__ushort_as_half((unsigned short)(in % 2 ? pair >> 16 : pair)));
+#pragma unroll
+                    for (int i = 0; i < TT; ++i)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) total[i][e] = __builtin_fmaf(f, part[i][e], total[i][e]);
+                }
+                ask_codes(next, k);
+                // as above: the requests stay here, one slice behind another
+                __builtin_amdgcn_sched_barrier(0);
             }
-            ask_codes(next, k);
-            // as above: the requests stay here, one slice behind another
-            __builtin_amdgcn_sched_barrier(0);
         }
         put_tokens(next, (p + 1) & 1);
         __syncthreads();
@@ -532,7 +538,7 @@ __global__ __launch_bounds__(NW *KG *kWave) void w4a16_grouped_parts_kernel(cons
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             const int t = 16 * i + 4 * q + e;
-            if (t < T && n < N) Y[(int64_t)t * ldy + n] = __float2half_rn(total[i][e]);
+            if (works && t < T && n < N) Y[(int64_t)t * ldy + n] = __float2half_rn(total[i][e]);
         }
 }
 
@@ -575,8 +581,9 @@ sq_status launch_grouped_parts(const GroupedArgs &a)
     auto kernel = w4a16_grouped_parts_kernel<GROUP, TT, NW, KG>;
     if (!allow_large_lds(reinterpret_cast<const void *>(kernel))) return SQ_ERR_LAUNCH;
     const int64_t blocks = ((int64_t)a.N + 15) / 16;
-    hipLaunchKernelGGL(kernel, dim3((unsigned)((blocks + NW - 1) / NW)), dim3(NW * KG * kWave), 2 * 16 * TT * kPartRow, a.st, a.X, a.ldx, a.T, a.K, a.Qw,
-                       a.steps, a.N, a.Y, a.ldy);
+    const int64_t rounds = (blocks + 256 * NW - 1) / (256 * NW), own = (blocks + 256 * rounds - 1) / (256 * rounds);       // of workgroups; blocks of one
+    hipLaunchKernelGGL(kernel, dim3((unsigned)((blocks + own - 1) / own)), dim3(NW * KG * kWave), 2 * 16 * TT * kPartRow, a.st, a.X, a.ldx, a.T, a.K,
+                       a.Qw, a.steps, a.N, a.Y, a.ldy, (int)own);
     return hipGetLastError() == hipSuccess ? SQ_OK : SQ_ERR_LAUNCH;
 }
 
@@ -590,13 +597,11 @@ sq_status launch_grouped_few(const GroupedArgs &a)
     // at more than one block of channels per workgroup (K = 11008, N = 4096 10.9 / 10.1).
     if (tiles == 1 && slices && large && (int64_t)a.T * row_bytes(a.K, 512) <= kMaxDynamicLds) return launch_grouped_rows<GROUP, 8, 4>(a);
     // In parts where they do not fit, or are more than 16 over a K worth the two barriers of a part (us, parts / the kernel for few
-    // tokens, groups of 128: T = 16, K = 8192, N = 28672 31.0 / 47.8, K = 5120, N = 13824 14.6 / 17.5, K = 8192, N = 8192 16.2 / 18.2, but
+    // tokens, groups of 128: T = 16, K = 8192, N = 28672 30.7 / 47.8, K = 5120, N = 13824 15.0 / 17.5, K = 8192, N = 8192 16.2 / 18.2, but
     // T = 8, K = 28672, N = 8192 42.1 / 39.3; T = 32, K = 1024, N = 28672 9.1 / 12.4, N = 16384 7.4 / 7.2; K = 2048, N = 16384 9.9 / 11.6;
-    // K = 4096, N = 8192 11.9 / 13.9).  Channels per workgroup: one round of workgroups again; groups of 32 and 64 want the waves.
+    // K = 4096, N = 8192 11.9 / 13.9).
     if (slices && blocks > 256 && (tiles == 2 ? a.K >= (blocks > 1024 ? 1024 : 2048) : large && (a.T > 8 || blocks > 512))) {
-        constexpr int KG = GROUP <= 64 ? 4 : 2;
-        if (blocks > 1024) return tiles == 2 ? launch_grouped_parts<GROUP, 2, 8, 2>(a) : launch_grouped_parts<GROUP, 1, 8, 2>(a);
-        if (blocks > 512) return tiles == 2 ? launch_grouped_parts<GROUP, 2, 4, KG>(a) : launch_grouped_parts<GROUP, 1, 4, KG>(a);
+        if (blocks > 512) return tiles == 2 ? launch_grouped_parts<GROUP, 2, 8, 2>(a) : launch_grouped_parts<GROUP, 1, 8, 2>(a);
         return tiles == 2 ? launch_grouped_parts<GROUP, 2, 2, 8>(a) : launch_grouped_parts<GROUP, 1, 2, 8>(a);
     }
     // The fewest channels per workgroup that need one round of workgroups on the 256 CUs (us with 16 / 32 / 64 channels, T = 1,
