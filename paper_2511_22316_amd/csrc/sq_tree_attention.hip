@@ -569,7 +569,9 @@ sq_status dispatch_tree_attention(const CacheView &c, AttentionCall &a, int64_t 
 extern "C" int64_t sq_tree_attention_workspace_bytes(int64_t T, int32_t Hq, int32_t D)
 {
     if (T < 0 || T > SQ_MAX_ROWS || Hq <= 0 || Hq > 65536 || (D != 64 && D != 128 && D != 256)) return -1;
-    return T * Hq * (int64_t)(D + 2) * 4 * 64;
+    // splits of all rows and heads together: a workgroup has 16 (32) rows and 1024 (512) of them are split at most
+    const int64_t sums = T * Hq < 256 ? T * Hq * sq::kMaxSplits : 16384;
+    return sums * (D + 2) * 4;
 }
 
 extern "C" sq_status sq_tree_attention(const void *Q, int64_t ldq, int64_t T, int32_t Hq, int32_t Hk, int32_t D,

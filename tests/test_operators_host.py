@@ -191,3 +191,10 @@ def test_host_tensors_are_refused(lib):
                  lambda: sq.sq_tree_attention(x, i(3), i(2), None, i(2, 2), 16, cache, 3, 0.1, x.clone())):
         with pytest.raises(ValueError, match="device"):
             call()
+
+
+def test_attention_workspace_is_bounded(lib):
+    size = sq.sq_tree_attention_workspace_bytes
+    assert size(1, 32, 128) == 64 * 32 * 130 * 4            # every split of the only row
+    assert size(256, 1, 64) == size(2048, 32, 64) == 16384 * 66 * 4
+    assert [size(T, 8, 256) for T in (1, 31, 32)] == [64 * T * 8 * 258 * 4 for T in (1, 31, 32)]
