@@ -20,27 +20,29 @@ __device__ __forceinline__ void rotation_of(int position, uint64_t turns, float 
     s *= magnitude;
 }
 
-// a c - b s with one rounding of b s and one of the sum, written out so that every kernel here gives the same bits
-__device__ __forceinline__ float turned_a(float a, float b, float c, float s) { return __builtin_fmaf(a, c, -(b * s)); }
-__device__ __forceinline__ float turned_b(float a, float b, float c, float s) { return __builtin_fmaf(b, c, a * s); }
-
-__device__ __forceinline__ uint32_t pack_halves(float a, float b)
+// a c - b s with one rounding of b s and one of the sum, which is then rounded to fp16: written out, and the sum kept from
+// being rounded to fp16 in the same instruction, so that every kernel here gives the same bits.
+__device__ __forceinline__ float rounded(float sum)
 {
-    const v2h p = {(_Float16)a, (_Float16)b};
-    return __builtin_bit_cast(uint32_t, p);
+    asm("" : "+v"(sum));
+    return sum;
 }
+__device__ __forceinline__ float turned_a(float a, float b, float c, float s) { return rounded(__builtin_fmaf(a, c, -(b * s))); }
+__device__ __forceinline__ float turned_b(float a, float b, float c, float s) { return rounded(__builtin_fmaf(b, c, a * s)); }
 
-// A lane owns one unit of 16 channels of a token's heads: eight pairs, channels 8 u .. and rot / 2 + 8 u .. (HALF) or
-// 16 u .. 16 u + 15.  It takes their cosines and sines once and then walks over the heads slot, slot + slots, ...  Behind
-// the rot / 16 units of pairs come units that are copied (none where Y is X); they go the same way as the others and keep
-// what they read, so a wave does not divide (8192 tokens, 40 heads of 128 with 64 turned: 44 us with a branch of their
-// own, 39.5 us so).  One read and one write of the rows: HBM-bound, 4.2 TB/s of both.
-template <bool HALF, bool COPIES>
+// A lane owns one unit of 2 V channels of a token's heads: V pairs, channels V u .. and rot / 2 + V u .. (HALF) or
+// 2 V u ..  It takes their cosines and sines once and then walks over the heads slot, slot + slots, ...  Behind the
+// rot / (2 V) units of pairs come units that are copied (none where Y is X); they go the same way as the others and keep what
+// they read, so a wave does not divide (8192 tokens, 40 heads of 128 with 64 turned: 44 us with a branch of their own,
+// 39.5 us so).  One read and one write of the rows: HBM-bound, 4.2 TB/s of both with V = 8.  V is the largest of 8, 4 and 2 that
+// the widths and strides allow (8192 tokens, 40 heads of 80: 40 turned 26.6 us, 20 26.3; a pair per lane took 82 and 92).
+template <int V, bool HALF, bool COPIES>
 __global__ __launch_bounds__(256) void rotary_kernel(const __half *X, int64_t T, int H, int D, int64_t ldx, int64_t ldh,
                                                      const int32_t *__restrict__ positions, const uint64_t *__restrict__ turns,
                                                      int rot, float magnitude, __half *Y, int64_t ldy, int64_t ldyh, int units,
                                                      int slots)
 {
+    typedef _Float16 Halves __attribute__((ext_vector_type(V)));
     const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x;
     const int per_token = units * slots;
     const int64_t t = id / per_token;
@@ -48,37 +50,38 @@ __global__ __launch_bounds__(256) void rotary_kernel(const __half *X, int64_t T,
     const int rest = (int)(id - t * per_token), u = rest % units, slot = rest / units;
     const __half *x = X + t * ldx;
     __half *y = Y + t * ldy;
-    const bool turned = !COPIES || u < rot / 16;
-    const int d0 = HALF && turned ? 8 * u : 16 * u, d1 = HALF && turned ? rot / 2 + 8 * u : d0 + 8;
-    const bool second = !COPIES || d1 < D;                            // the last copied unit may be half a unit
+    const bool turned = !COPIES || u < rot / (2 * V);
+    const int d0 = HALF && turned ? V * u : 2 * V * u, d1 = HALF && turned ? rot / 2 + V * u : d0 + V;
+    const bool second = !COPIES || d1 < D;                 // the last copied unit may be half a unit
     const int d2 = second ? d1 : d0;
-    float c[8] = {}, s[8] = {};
+    float c[V] = {}, s[V] = {};
     if (turned) {                                          // without turned channels there is no table, and no position is read
         const int position = positions[t];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) rotation_of(position, turns[8 * u + e], magnitude, c[e], s[e]);
+        for (int e = 0; e < V; ++e) rotation_of(position, turns[V * u + e], magnitude, c[e], s[e]);
     }
 #pragma unroll 4
     for (int h = slot; h < H; h += slots) {
-        const uint4 p = *reinterpret_cast<const uint4 *>(x + h * ldh + d0), q = *reinterpret_cast<const uint4 *>(x + h * ldh + d2);
-        const v8h a = __builtin_bit_cast(v8h, p), b = __builtin_bit_cast(v8h, q);
-        uint32_t wa[4], wb[4];
+        const Halves a = *reinterpret_cast<const Halves *>(x + h * ldh + d0), b = *reinterpret_cast<const Halves *>(x + h * ldh + d2);
+        Halves ya, yb;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
+        for (int j = 0; j < V; ++j) {
             if constexpr (HALF) {
-                const int e = 2 * j, f = 2 * j + 1;
-                wa[j] = pack_halves(turned_a(a[e], b[e], c[e], s[e]), turned_a(a[f], b[f], c[f], s[f]));
-                wb[j] = pack_halves(turned_b(a[e], b[e], c[e], s[e]), turned_b(a[f], b[f], c[f], s[f]));
-            } else {
-                const int e = 2 * j, f = 2 * j + 1;        // pairs j of the unit's first eight channels and 4 + j
-                wa[j] = pack_halves(turned_a(a[e], a[f], c[j], s[j]), turned_b(a[e], a[f], c[j], s[j]));
-                wb[j] = pack_halves(turned_a(b[e], b[f], c[4 + j], s[4 + j]), turned_b(b[e], b[f], c[4 + j], s[4 + j]));
+                ya[j] = (_Float16)turned_a(a[j], b[j], c[j], s[j]);
+                yb[j] = (_Float16)turned_b(a[j], b[j], c[j], s[j]);
+            } else {                                       // pairs of the unit's first V channels, then of the others
+                const int e = j & ~1, f = e + 1, at = j / 2, bt = V / 2 + at;
+                ya[j] = (_Float16)(j == e ? turned_a(a[e], a[f], c[at], s[at]) : turned_b(a[e], a[f], c[at], s[at]));
+                yb[j] = (_Float16)(j == e ? turned_a(b[e], b[f], c[bt], s[bt]) : turned_b(b[e], b[f], c[bt], s[bt]));
             }
         }
-        const uint4 ya = {turned ? wa[0] : p.x, turned ? wa[1] : p.y, turned ? wa[2] : p.z, turned ? wa[3] : p.w};
-        const uint4 yb = {turned ? wb[0] : q.x, turned ? wb[1] : q.y, turned ? wb[2] : q.z, turned ? wb[3] : q.w};
-        *reinterpret_cast<uint4 *>(y + h * ldyh + d0) = ya;
-        if (second) *reinterpret_cast<uint4 *>(y + h * ldyh + d1) = yb;
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+            ya[j] = turned ? ya[j] : a[j];
+            yb[j] = turned ? yb[j] : b[j];
+        }
+        *reinterpret_cast<Halves *>(y + h * ldyh + d0) = ya;
+        if (second) *reinterpret_cast<Halves *>(y + h * ldyh + d1) = yb;
     }
 }
 
@@ -104,6 +107,25 @@ __global__ __launch_bounds__(256) void rotary_pair_kernel(const __half *X, int64
     const float a = __half2float(x[p]), b = __half2float(x[q]);
     y[p] = __float2half_rn(turned_a(a, b, c, s));
     y[q] = __float2half_rn(turned_b(a, b, c, s));
+}
+
+template <int V>
+sq_status launch_rotary(const __half *x, int64_t T, int H, int D, int64_t ldx, int64_t ldh, const int32_t *positions, const uint64_t *turns,
+                        int rot, bool half, float magnitude, __half *y, int64_t ldy, int64_t ldyh, int copied, hipStream_t st)
+{
+    const int units = rot / (2 * V) + (copied + 2 * V - 1) / (2 * V);
+    // enough lanes that every SIMD of the chip holds four waves, and at least eight heads side by side in a row
+    const int64_t lanes = T * (int64_t)units;
+    int64_t want = (262144 + lanes - 1) / lanes;
+    if (want < 8) want = 8;
+    const int slots = (int)(want < H ? want : H);
+    const int64_t blocks = (lanes * slots + 255) / 256;
+    if (blocks > 0x7FFFFFFF) return SQ_ERR_SHAPE;
+    auto kernel = half ? (copied ? rotary_kernel<V, true, true> : rotary_kernel<V, true, false>)
+                       : (copied ? rotary_kernel<V, false, true> : rotary_kernel<V, false, false>);
+    hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(256), 0, st, x, T, H, D, ldx, ldh, positions, turns, rot, magnitude, y, ldy, ldyh, units,
+                       slots);
+    return hipGetLastError() == hipSuccess ? SQ_OK : SQ_ERR_LAUNCH;
 }
 
 }  // namespace
@@ -158,27 +180,17 @@ extern "C" sq_status sq_rotary_fp16(const void *X, int64_t T, int32_t H, int32_t
     hipStream_t st = static_cast<hipStream_t>(stream);
     const int copied = in_place ? 0 : D - rot;
     if (rot == 0 && copied == 0) return SQ_OK;
-    const bool wide = (rot % 16) == 0 && (D % 8) == 0 && (ldx % 8) == 0 && (ldh % 8) == 0 && (ldy % 8) == 0 && (ldyh % 8) == 0 &&
-                      ((uintptr_t)X & 15) == 0 && ((uintptr_t)Y & 15) == 0;
-    if (wide) {
-        const int units = rot / 16 + (copied + 15) / 16;
-        // enough lanes that every SIMD of the chip holds four waves, and at least eight heads side by side in a row
-        const int64_t lanes = T * (int64_t)units;
-        int64_t want = (262144 + lanes - 1) / lanes;
-        if (want < 8) want = 8;
-        const int slots = (int)(want < H ? want : H);
-        const int64_t blocks = (lanes * slots + 255) / 256;
-        if (blocks > 0x7FFFFFFF) return SQ_ERR_SHAPE;
-        auto kernel = half ? (copied ? sq::rotary_kernel<true, true> : sq::rotary_kernel<true, false>)
-                           : (copied ? sq::rotary_kernel<false, true> : sq::rotary_kernel<false, false>);
-        hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(256), 0, st, x, T, H, D, ldx, ldh, positions, turns, rot, magnitude,
-                           y, ldy, ldyh, units, slots);
-    } else {
-        const int units = rot / 2 + copied;
-        const int64_t blocks = (T * H * units + 255) / 256;
-        if (blocks > 0x7FFFFFFF) return SQ_ERR_SHAPE;
-        hipLaunchKernelGGL(sq::rotary_pair_kernel, dim3((unsigned)blocks), dim3(256), 0, st, x, T, H, D, ldx, ldh, positions, turns,
-                           rot, half, magnitude, y, ldy, ldyh, units);
-    }
+    // units of 2 V channels need every place of them on a multiple of V
+    auto places = [&](int V) {
+        return rot % (2 * V) == 0 && ((int64_t)D | ldx | ldh | ldy | ldyh) % V == 0 && (((uintptr_t)X | (uintptr_t)Y) & (2 * V - 1)) == 0;
+    };
+    if (places(8)) return sq::launch_rotary<8>(x, T, H, D, ldx, ldh, positions, turns, rot, half, magnitude, y, ldy, ldyh, copied, st);
+    if (places(4)) return sq::launch_rotary<4>(x, T, H, D, ldx, ldh, positions, turns, rot, half, magnitude, y, ldy, ldyh, copied, st);
+    if (places(2)) return sq::launch_rotary<2>(x, T, H, D, ldx, ldh, positions, turns, rot, half, magnitude, y, ldy, ldyh, copied, st);
+    const int units = rot / 2 + copied;
+    const int64_t blocks = (T * H * units + 255) / 256;
+    if (blocks > 0x7FFFFFFF) return SQ_ERR_SHAPE;
+    hipLaunchKernelGGL(sq::rotary_pair_kernel, dim3((unsigned)blocks), dim3(256), 0, st, x, T, H, D, ldx, ldh, positions, turns, rot, half,
+                       magnitude, y, ldy, ldyh, units);
     return hipGetLastError() == hipSuccess ? SQ_OK : SQ_ERR_LAUNCH;
 }

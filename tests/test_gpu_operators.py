@@ -784,3 +784,33 @@ def test_product_in_parts(T, K, N, group):
     got = run_product(X, codes, steps)
     assert (got[T - 1].astype(np.float64) == np.inf * codes[:, K - 1]).all()
     ou.held(got[: T - 1], want[: T - 1], bound[: T - 1], "others")
+
+
+@pytest.mark.parametrize("half", [False, True])
+@pytest.mark.parametrize("T,H,D,rot", [(40, 5, 80, 40), (33, 6, 96, 24), (5, 3, 20, 8), (9, 2, 36, 12), (3, 2, 10, 4), (1000, 9, 80, 20), (6, 3, 44, 40)])
+def test_rotary_narrow_units(T, H, D, rot, half):
+    """Widths that go in units of 2, 4 or 8 pairs, and the same rows at places that allow fewer: the same bits."""
+    import torch
+    import paper_2511_22316_amd as sq
+    print(f"case rotary units {T} {H} {D} {rot} {half}", flush=True)
+    g = rng(17, T, H, D, rot)
+    X = rows(g, T, H * D).reshape(T, H, D)
+    pos = g.integers(0, 2 ** 20, T).astype(np.int32)
+    turns = sq.sq_rotary_table(rot).cuda()
+    want, bound = ou.rotary(X, pos, ou.frequencies(rot), half, 1.0)
+    got = None
+    for at, row in ((0, 0), (4, 4), (2, 6), (1, 3)):        # halves in front of the rows and behind each
+        buf = torch.full((at + T * (H * D + row) + 8,), 3.0, dtype=torch.float16, device="cuda")
+        out = buf.clone()
+        view = lambda b: b[at: at + T * (H * D + row)].view(T, H * D + row)[:, : H * D].unflatten(1, (H, D))     # noqa: E731
+        view(buf)[:] = dev(X)
+        sq.sq_rotary_fp16(view(buf), dev(pos), turns, half, view(out))
+        sq.sq_rotary_fp16(view(buf), dev(pos), turns, half, view(buf))
+        assert torch.equal(out, buf)                        # in place and beside, and nothing around them
+        y = host(view(out).contiguous())
+        if got is None:
+            ou.held(y, want, bound, "units")
+            got = y
+        assert np.array_equal(y, got)
+        view(out)[:] = 3.0
+        assert (out == 3.0).all()
