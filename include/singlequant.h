@@ -444,7 +444,7 @@ sq_status sq_quantize_grouped(const void *X, int64_t T, int32_t K, int64_t ldx,
  * Requires K % 64 == 0, K % group == 0, K <= 131072, T <= 2^24.  T == 0 or N == 0
  * is legal and enqueues nothing.
  * At most 32 tokens: the sum of a group is exact products in fp32, then scaled in
- * fp32.  More tokens: code * step is rounded to fp16 first (at most half a step of
+ * fp32.  More tokens: code * step may be rounded to fp16 first (at most half a step of
  * fp16, and steps beyond 8188 may make it infinite), sums in fp32.  The order of the
  * additions goes with the sizes, and at most 32 tokens with the output channel's
  * number too.

@@ -600,7 +600,7 @@ sq_status launch_grouped_few(const GroupedArgs &a)
     // tokens, groups of 128: T = 16, K = 8192, N = 28672 30.7 / 47.8, K = 5120, N = 13824 15.0 / 17.5, K = 8192, N = 8192 16.2 / 18.2, but
     // T = 8, K = 28672, N = 8192 42.1 / 39.3; T = 32, K = 1024, N = 28672 9.1 / 12.4, N = 16384 7.4 / 7.2; K = 2048, N = 16384 9.9 / 11.6;
     // K = 4096, N = 8192 11.9 / 13.9).
-    if (slices && blocks > 256 && (tiles == 2 ? a.K >= (blocks > 1024 ? 1024 : 2048) : large && (a.T > 8 || blocks > 512))) {
+    if (slices && blocks > 256 && (tiles == 2 ? a.K >= (blocks > 1024 ? 1024 : 2048) : tiles == 1 && large && (a.T > 8 || blocks > 512))) {
         if (blocks > 512) return tiles == 2 ? launch_grouped_parts<GROUP, 2, 8, 2>(a) : launch_grouped_parts<GROUP, 1, 8, 2>(a);
         return tiles == 2 ? launch_grouped_parts<GROUP, 2, 2, 8>(a) : launch_grouped_parts<GROUP, 1, 2, 8>(a);
     }
@@ -615,7 +615,7 @@ sq_status launch_grouped_few(const GroupedArgs &a)
 }
 
 // Many tokens: the tile kernel of sq_w4a16_gemm with the steps on the widened codes.  Us per shape, groups of 128:
-//   64 x 128, two K groups    T = 333, K = N = 4096 26; up to 64 tokens in any case (K = 8192, N = 57344 108)
+//   64 x 128, two K groups    T = 333, K = N = 4096 26; 64 tokens in any case (K = 8192, N = 57344 108)
 //   128 x 128, two K groups   T = 333, K = N = 4096 33; T = 333, N = 9000 38.5 (64 x 128 45.6); T = 1000, N = 4096 44 (53)
 //   128 x 256                 T = 333, K = N = 4096 47; T = 600, N = 9000 56 (128 x 128 73); T = 64, K = 8192, N = 57344 120
 //   256 x 256                 1.85 times as long per round of 256 workgroups as 128 x 256, over seven shapes, so it is taken where
@@ -653,7 +653,10 @@ extern "C" sq_status sq_w4a16_gemm_grouped(const void *X, int64_t T, int32_t K, 
         return SQ_ERR_ALIGN;
     const sq::GroupedArgs a = {static_cast<const __half *>(X), ldx, (int)T, K, Qw, static_cast<const __half *>(steps), group, N,
                                static_cast<__half *>(Y), ldy, static_cast<hipStream_t>(stream)};
-    if (T > 32) return sq::launch_grouped_many(a);
+    // Tiles of many tokens, but where the kernel for few needs one round of workgroups for them all: a workgroup there shares K
+    // among eight waves, a tile is one walk over it (us, few / tiles, groups of 128: T = 64, K = 4096, N = 1024 7.8 / 23.8, T = 128,
+    // N = 4096 19.4 / 24.4, K = 11008 38.8 / 62.9; two rounds: T = 48, N = 11008 33.3 / 26.1, T = 128, N = 8192 35.7 / 25.4).
+    if (T > 32 && (T + 31) / 32 * (((int64_t)N + 63) / 64) > 256) return sq::launch_grouped_many(a);
     if (group == 32) return sq::launch_grouped_few<32>(a);
     if (group == 64) return sq::launch_grouped_few<64>(a);
     if (group == 128) return sq::launch_grouped_few<128>(a);

@@ -814,3 +814,13 @@ def test_rotary_narrow_units(T, H, D, rot, half):
         assert np.array_equal(y, got)
         view(out)[:] = 3.0
         assert (out == 3.0).all()
+
+
+@pytest.mark.parametrize("T,K,N,group", [(33, 256, 1000, 64), (64, 384, 1500, 128), (100, 320, 2000, 64), (200, 256, 2040, 32), (2000, 128, 200, 128),
+                                         (64, 320, 16384, 32), (65, 320, 16384, 32), (500, 192, 5000, 64), (700, 256, 6000, 32)])
+def test_product_between_few_and_many(T, K, N, group):
+    print(f"case product {T} {K} {N} {group}", flush=True)
+    g = rng(18, T, K, N, group)
+    X, (codes, steps) = rows(g, T, K), weights(g, N, K, group)
+    want, bound = ou.product(X, codes, steps, group, True)
+    ou.held(run_product(X, codes, steps, 8, 3), want, bound, f"{T} {K} {N} {group}")

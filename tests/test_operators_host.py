@@ -198,3 +198,8 @@ def test_attention_workspace_is_bounded(lib):
     assert size(1, 32, 128) == 64 * 32 * 130 * 4            # every split of the only row
     assert size(256, 1, 64) == size(2048, 32, 64) == 16384 * 66 * 4
     assert [size(T, 8, 256) for T in (1, 31, 32)] == [64 * T * 8 * 258 * 4 for T in (1, 31, 32)]
+
+
+def test_grouped_steps_of_groups_of_32_are_read_in_pairs(lib):
+    call = lambda group, s: lib.sq_w4a16_gemm_grouped(FAKE, 4, 256, 256, FAKE, s, group, 8, FAKE, 8, None)       # noqa: E731
+    assert call(32, FAKE + 2) == ALIGN and call(32, FAKE + 1) == ALIGN and call(64, FAKE + 1) == ALIGN
