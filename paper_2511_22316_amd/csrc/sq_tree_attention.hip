@@ -545,14 +545,19 @@ sq_status dispatch_tree_attention(const CacheView &c, AttentionCall &a, int64_t 
     const int64_t blocks_of_16 = (rows + 15) / 16 * c.Hk * c.B;
     const int64_t per_block = D < 256 && rows > 16 && (double)blocks_of_16 * (double)max_keys > 0x1p20 ? 32 : 16;
     a.row_blocks = (int)((rows + per_block - 1) / per_block);
-    // As many splits as keep the workgroups within the four (R = 2: two) that a CU holds (a few more would make a second
-    // round), chunks of at least 128 keys, and what the workspace holds.  (us at 48 sequences of 8192 keys, 8 heads: two splits, 768 workgroups,
-    // 95; three, 1152 of them, 111; 16 trees, 1536 workgroups of 16 rows without a split 107, with two 151.)
-    const int64_t units = (int64_t)a.row_blocks * c.Hk * c.B;
-    int64_t splits = (per_block == 32 ? 512 : 1024) / units;
+    // Splits of the keys: as many as give every CU a workgroup, twice (four times, of many units) that while a split has 2048 keys
+    // or more, no more than there are chunks of 128 keys, and none where the keys' tiles take less time than the second launch,
+    // about 3 us (us without a split / best / 1024 workgroups, one row of 32 heads per sequence, 8 of K and V, D = 128: one sequence
+    // of 512 keys 6.9 / 7.7 / 7.7, of 1024 9.5 / 7.8 / 7.8, of 16384 92 / 11.7 / 13.0; 4 of 4096 26.7 / 11.6 with 8 / 13.5, of 16384
+    // 93 / 19.0 with 16 / 20.8; 16 of 1024 10.5 / 11.8 with 2 / 13.3, of 4096 26.9 / 19.5 with 4 / 21.3; 48 of 4096 to 8192 74.2 / 70.6
+    // with 2).  And no more than the workspace holds.
+    const int64_t units = (int64_t)a.row_blocks * c.Hk * c.B, most = units > 256 && per_block == 16 ? 1024 : 512;
     const int64_t chunks = (max_keys + kChunkUnit - 1) / kChunkUnit, room = workspace_bytes / (a.T * a.Hq * (D + 2) * 4);
+    int64_t splits = units < 256 ? 256 / units : 1;
+    while (2 * splits * units <= most && max_keys >= 2048 * splits) splits *= 2;
     splits = splits < chunks ? splits : chunks;
     splits = splits < kMaxSplits ? splits : kMaxSplits;
+    if (max_keys * (splits - 1) < 590 * splits) splits = 1;
     splits = splits < room ? splits : room;
     a.splits = splits < 1 ? 1 : (int)splits;
     a.part = static_cast<float *>(workspace);

@@ -824,3 +824,15 @@ def test_product_between_few_and_many(T, K, N, group):
     X, (codes, steps) = rows(g, T, K), weights(g, N, K, group)
     want, bound = ou.product(X, codes, steps, group, True)
     ou.held(run_product(X, codes, steps, 8, 3), want, bound, f"{T} {K} {N} {group}")
+
+
+@pytest.mark.parametrize("Hq,Hk,D,page,new,tree", [(8, 2, 64, 16, [1, 1, 1, 1], False), (4, 4, 128, 64, [1, 0, 1, 1], False), (6, 2, 256, 32, [1, 1, 1, 1], False),
+                                                   (8, 1, 128, 16, [9, 3, 1, 17], True), (5, 1, 64, 128, [2, 7, 4, 1], False)])
+def test_attention_of_split_sequences(Hq, Hk, D, page, new, tree):
+    print(f"case attention split {Hq} {Hk} {D} {page} {new} {tree}", flush=True)
+    s = Setting(1100 + D + page, [2500, 900, 0, 3000], new, Hk, D, page)
+    Q, scale = s.queries(Hq, 2.0), D ** -0.5
+    words = s.trees() if tree else None
+    want, bound = s.expect(Q, Hq // Hk, s.by_mask(words) if tree else s.causal, scale)
+    for max_keys in (None, 3000, 8000):
+        ou.held(s.run(Q, words, scale, max_keys=max_keys), want, bound, f"{max_keys}")
