@@ -488,6 +488,19 @@ def _heads(t, name, packed=True):
     return T, H, D, row, head
 
 
+def _two_heads(a, a_name, b, b_name):
+    """Two tensors of one shape as _heads takes them: the shape and both row strides."""
+    shape = a.shape
+    if b.shape != shape:
+        raise ValueError(f"{a_name} and {b_name} must have the same shape")
+    T, H, D = shape
+    row, head, one = a.stride()
+    b_row, b_head, b_one = b.stride()
+    if head == D == b_head and one == 1 == b_one and row >= H * D <= b_row and a.dtype is _f16 and b.dtype is _f16:
+        return T, H, D, row, b_row                         # the usual layout, without the calls
+    return T, H, D, _heads(a, a_name)[3], _heads(b, b_name)[3]
+
+
 def _here(stream, *tensors):
     """The stream to work on; the tensors must be on the current device (a kernel that follows a host pointer takes the
     process down, and sq_rotary_table's result is one that has to be copied)."""
@@ -592,10 +605,7 @@ def sq_cache_append(K, V, row_start, cached, table, page, cache, stream=None) ->
     """New rows K, V fp16 [T, Hk, D] (any row strides) into the cache: row_start int32 [B + 1], cached int32 [B], table
     int32 [B, pages of a sequence], cache uint8, pages * sq_cache_page_bytes(Hk, D, page) bytes."""
     lib = _lib or _load()
-    T, Hk, D, ldk, _ = _heads(K, "K")
-    ldv = _heads(V, "V")[3]
-    if V.shape != K.shape:
-        raise ValueError("K and V must have the same shape")
+    T, Hk, D, ldk, ldv = _two_heads(K, "K", V, "V")
     B, per_sequence, pages = _cache_args(Hk, D, row_start, cached, table, page, cache)
     code = lib.sq_cache_append(K.data_ptr(), ldk, V.data_ptr(), ldv, T, Hk, D, row_start.data_ptr(), cached.data_ptr(), B,
                                table.data_ptr(), per_sequence, page, cache.data_ptr(), pages,
@@ -607,10 +617,7 @@ def sq_cache_append(K, V, row_start, cached, table, page, cache, stream=None) ->
 def sq_cache_read(cache, row_start, cached, table, page, K, V, stream=None) -> None:
     """The rows that sq_cache_append with the same arrays writes, as fp16 into K, V [T, Hk, D]."""
     lib = _lib or _load()
-    T, Hk, D, ldk, _ = _heads(K, "K")
-    ldv = _heads(V, "V")[3]
-    if V.shape != K.shape:
-        raise ValueError("K and V must have the same shape")
+    T, Hk, D, ldk, ldv = _two_heads(K, "K", V, "V")
     B, per_sequence, pages = _cache_args(Hk, D, row_start, cached, table, page, cache)
     code = lib.sq_cache_read(cache.data_ptr(), pages, Hk, D, row_start.data_ptr(), cached.data_ptr(), B, table.data_ptr(),
                              per_sequence, page, K.data_ptr(), ldk, V.data_ptr(), ldv, T,
@@ -629,10 +636,7 @@ def sq_tree_attention(Q, row_start, cached, mask, table, page, cache, Hk, scale,
     row j of its sequence) or None (rows 0 .. i); max_rows: at least the new rows of every sequence; max_keys: about the
     longest sequence (None: what the table holds); workspace: any contiguous device tensor, or None (nothing is split)."""
     lib = _lib or _load()
-    T, Hq, D, ldq, _ = _heads(Q, "Q")
-    ldo = _heads(O, "O")[3]
-    if O.shape != Q.shape:
-        raise ValueError("O must have the shape of Q")
+    T, Hq, D, ldq, ldo = _two_heads(Q, "Q", O, "O")
     B, per_sequence, pages = _cache_args(Hk, D, row_start, cached, table, page, cache)
     if mask is not None and (mask.dtype is not _i64 or not mask.is_contiguous() or mask.numel() != T):
         raise ValueError("mask must be int64, one word per row")
