@@ -482,9 +482,10 @@ sq_status sq_w4a16_gemm_grouped(const void *X, int64_t T, int32_t K, int64_t ldx
  *   X, Y       device, fp16; head h of token t begins at t * ldx + h * ldh (Y: ldy,
  *              ldyh) and has D channels; ldh >= D, ldx >= (H - 1) ldh + D.  Y may be
  *              X with the same strides (in place: the channels behind `rot` are not
- *              touched); any other overlap is an error of the caller.  Multiples of
- *              8 for D and the strides, 16 for rot, and 16-byte aligned pointers make
- *              it fast; nothing but 2-byte alignment is required.
+ *              touched); any other overlap is an error of the caller.  Nothing but
+ *              2-byte alignment is required; it is fast where D, rot / 2, the strides
+ *              and the pointers' distance from 0 in channels are even, and best where
+ *              they are multiples of 8.
  *   positions  device, int32 [T], any value
  *   turns      device, uint64 [rot / 2]
  *   rot        even, 0 .. D; half 0 or 1; magnitude: 1 unless the scaling asks for

@@ -836,3 +836,95 @@ def test_attention_of_split_sequences(Hq, Hk, D, page, new, tree):
     want, bound = s.expect(Q, Hq // Hk, s.by_mask(words) if tree else s.causal, scale)
     for max_keys in (None, 3000, 8000):
         ou.held(s.run(Q, words, scale, max_keys=max_keys), want, bound, f"{max_keys}")
+
+
+def test_calls_without_work():
+    import torch
+    import paper_2511_22316_amd as sq
+    print("case empty calls", flush=True)
+    h = lambda *n: torch.full(n, 3.0, dtype=torch.float16, device="cuda")       # noqa: E731
+    u = lambda *n: torch.zeros(n, dtype=torch.uint8, device="cuda")             # noqa: E731
+    i = lambda *n: torch.zeros(n, dtype=torch.int32, device="cuda")             # noqa: E731
+    turns = sq.sq_rotary_table(32).cuda()
+    sq.sq_quantize_grouped(h(0, 64), 32, u(0, 32), h(0, 2))
+    sq.sq_w4a16_gemm_grouped(h(0, 64), u(5, 32), h(5, 2), h(0, 5))
+    sq.sq_w4a16_gemm_grouped(h(3, 64), u(0, 32), h(0, 2), h(3, 0))
+    sq.sq_rotary_fp16(h(0, 3, 64), i(0), turns, True, h(0, 3, 64))
+    sq.sq_rotary_fp16(h(2, 0, 64), i(2), turns, True, h(2, 0, 64))
+    size = sq.sq_cache_page_bytes(2, 64, 16)
+    for B, T, per, pages in ((0, 0, 0, 0), (0, 0, 2, 3), (2, 0, 1, 3), (2, 4, 0, 3), (2, 4, 2, 0)):
+        start = dev(np.array([0, 1, T][: B] + [T], np.int32)) if B else i(1)
+        table, cache, k, v, o = torch.full((B, per), -1, dtype=torch.int32, device="cuda"), u(pages, size), h(T, 2, 64), h(T, 2, 64), h(T, 4, 64)
+        sq.sq_cache_append(k, v, start, i(B), table, 16, cache)
+        sq.sq_cache_read(cache, start, i(B), table, 16, k, v)
+        sq.sq_tree_attention(h(T, 4, 64), start, i(B), None, table, 16, cache, 2, 0.1, o, max_rows=4)
+        torch.cuda.synchronize()
+        assert (k == 3).all() and (v == 3).all() and not cache.any()
+        assert (o == 0).all()                               # rows of a sequence without keys
+
+
+def test_cache_read_into_parts_of_rows_and_shared_pages():
+    """Two sequences with the same first pages, read and attended to; K and V are written into wider rows."""
+    import torch
+    import paper_2511_22316_amd as sq
+    print("case shared pages", flush=True)
+    s = Setting(1200, [64, 64], [1, 1], 2, 128, 32)
+    s.table[1, :2] = s.table[0, :2]                         # the pages of the 64 old rows
+    table = dev(s.table)
+    s.numbers.rows[1][0][:64] = s.numbers.rows[0][0][:64]
+    s.numbers.rows[1][1][:64] = s.numbers.rows[0][1][:64]
+    Q = s.queries(8)
+    want, bound = s.expect(Q, 4, s.causal, 0.1)
+    ou.held(s.run(Q, None, 0.1, table=s.table), want, bound, "shared")
+    buf = torch.full((2, 2 * 256 + 16), 3.0, dtype=torch.float16, device="cuda")
+    k, v = buf[:, :256].unflatten(1, (2, 128)), buf[:, 264: 264 + 256].unflatten(1, (2, 128))
+    sq.sq_cache_read(s.cache, s.dstart, s.dcached, table, 32, k, v)
+    for b in range(2):
+        assert np.array_equal(host(k)[b], s.numbers.values(b, 0, 65)[0][64].astype(np.float16))
+        assert np.array_equal(host(v)[b], s.numbers.values(b, 1, 65)[0][64].astype(np.float16))
+    assert (buf[:, 256: 264] == 3).all() and (buf[:, 520:] == 3).all()
+
+
+def test_two_streams_at_once():
+    """The same calls on two streams, each with a cache and a workspace of its own, against one after the other."""
+    import torch
+    import paper_2511_22316_amd as sq
+    print("case two streams", flush=True)
+    g = rng(21)
+    B, Hq, Hk, D, page, K = 4, 8, 2, 128, 64, 512
+    W = (Hq + 2 * Hk) * D
+    codes, steps = weights(g, W, K, 128)
+    Qw, sw, turns = dev(ou.pack(codes)), dev(steps), sq.sq_rotary_table(D).cuda()
+    start, table = dev(np.arange(B + 1, dtype=np.int32)), dev(np.arange(B * 20, dtype=np.int32).reshape(B, 20))
+    cached = dev(np.array([1000, 1100, 1200, 900], np.int32))
+    filled = torch.randint(0, 256, (B * 20, sq.sq_cache_page_bytes(Hk, D, page)), dtype=torch.uint8, device="cuda")
+    filled.view(torch.float16)[:, Hk * page * D // 2:] = 0.05
+    X = [dev(rows(g, B, K)) for _ in range(2)]
+
+    def step(n, stream):
+        cache, qkv = filled.clone(), torch.empty(B, W, dtype=torch.float16, device="cuda")
+        O, ws = torch.empty(B, Hq, D, dtype=torch.float16, device="cuda"), torch.empty(4 << 20, dtype=torch.uint8, device="cuda")
+        torch.cuda.synchronize()
+        def go():
+            for _ in range(20):
+                sq.sq_w4a16_gemm_grouped(X[n], Qw, sw, qkv, stream=stream)
+                heads = qkv.unflatten(1, (Hq + 2 * Hk, D))
+                qk = heads[:, : Hq + Hk]
+                sq.sq_rotary_fp16(qk, cached, turns, True, qk, stream=stream)
+                sq.sq_cache_append(qk[:, Hq:], heads[:, Hq + Hk:], start, cached, table, page, cache, stream=stream)
+                sq.sq_tree_attention(qk[:, :Hq], start, cached, None, table, page, cache, Hk, D ** -0.5, O, ws, stream=stream)
+        return go, (cache, qkv, O)
+
+    alone = []
+    for n in range(2):
+        go, out = step(n, None)
+        go()
+        torch.cuda.synchronize()
+        alone.append([t.clone() for t in out])
+    both = [step(n, torch.cuda.Stream()) for n in range(2)]
+    for go, _ in both:
+        go()
+    torch.cuda.synchronize()
+    for (_, out), want in zip(both, alone):
+        assert all(torch.equal(a, b) for a, b in zip(out, want))
+    assert not torch.equal(alone[0][2], alone[1][2])
