@@ -132,7 +132,8 @@ __global__ __launch_bounds__(kWaves *kWave, D == 256 || R == 2 ? 2 : 4) void tre
     const int lane = threadIdx.x & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
     const int l16 = lane & 15, q = lane >> 4;
     int id = xcd_contiguous_id((int)blockIdx.x, (int)gridDim.x);
-    const int row_block = id % a.row_blocks;
+    // of a prompt's rows the last ones see the most: they start first (4096 rows 221 -> 214 us; of a tree all see about the same)
+    const int row_block = a.mask ? id % a.row_blocks : a.row_blocks - 1 - id % a.row_blocks;
     id /= a.row_blocks;
     const int split = id % a.splits;
     id /= a.splits;
