@@ -519,7 +519,7 @@ sq_status sq_rotary_fp16(const void *X, int64_t T, int32_t H, int32_t D, int64_t
  *   - per head `page` D bytes: the codes of K, row after row (D / 2 bytes each), then
  *     those of V in blocks of 16 rows, in a block [row / 4 % 4][unit][row % 4], a unit
  *     being D / 16 neighbouring channels (unit u: channels u D / 16 ..);
- *   - then the steps, fp16: K [Hk][page], V [Hk][page].
+ *   - then the steps, fp16, above 0 and finite: K [Hk][page], V [Hk][page].
  *
  * Sequence b of B owns the new rows row_start[b] .. row_start[b + 1] - 1 of the
  * call's T rows; they follow the cached[b] rows it has already, and its row number p

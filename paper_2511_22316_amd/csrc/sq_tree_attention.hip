@@ -88,8 +88,9 @@ __device__ __forceinline__ int by_length(const CacheView &c, const AttentionCall
 // A workgroup takes one head of K and V of one sequence, 16 R query rows (row = new row * group + query head in the group)
 // and every splits-th chunk of its keys; its four waves take every fourth tile of 32 keys each and work alone until
 // the end.  What it does per key, whatever the rows, is most of the work of 16 of them (widening the codes: 120 of 260
-// instructions), so more rows are taken 32 at a time (R = 2) where there is enough to do, at half the waves per SIMD: the trees above 116 -> 94 us,
-// prompts of 256 to 512 rows 189 -> 128.  Neighbouring workgroups belong to an XCD and have a head of many sequences.
+// instructions), so more rows are taken 32 at a time (R = 2) where there is enough to do: the trees above 116 -> 94 us, prompts of
+// 256 to 512 rows 189 -> 128.  Their query rows stay in LDS, so that three waves fit on a SIMD (four prompts of 2048 rows
+// 251 us with two, 225 so).  Neighbouring workgroups belong to an XCD and have a head of many sequences.
 //
 // Scores: S^T = K Q^T on v_mfma_f32_16x16x32_f16, the keys as rows of the result and the query rows as columns, so a lane has
 // one query row (lane % 16) and four keys of each half of the tile (4 (lane / 16) + r); the weights it makes of them are
@@ -118,7 +119,7 @@ __device__ __forceinline__ int by_length(const CacheView &c, const AttentionCall
 // only.  The page numbers are requested a tile ahead of that.
 // ONE_PAGE: pages of 32 rows and more, a tile lies in one.
 template <int D, bool ONE_PAGE, int R>
-__global__ __launch_bounds__(kWaves *kWave, D == 256 || R == 2 ? 2 : 4) void tree_attention_kernel(const CacheView c, const AttentionCall a)
+__global__ __launch_bounds__(kWaves *kWave, D == 256 ? 2 : R == 2 ? 3 : 4) void tree_attention_kernel(const CacheView c, const AttentionCall a)
 {
     constexpr int KD = D / 32;                       // dwords of K (and of V) per lane and 16 keys; steps of the scores
     constexpr int VT = D / 16;                       // 16-channel tiles of the output
@@ -126,6 +127,7 @@ __global__ __launch_bounds__(kWaves *kWave, D == 256 || R == 2 ? 2 : 4) void tre
     constexpr int NS = 2, STAGE = 32 * D + 128, PIECES = D / 64, LOADS = 2 * PIECES + 1;      // K, V, steps of a tile
     constexpr int MEET = kWaves * 16 * (LD * 4 + 8), RING = kWaves * NS * STAGE;
     __shared__ uint4 shared_u4[(RING > MEET ? RING : MEET) / 16];
+    __shared__ uint4 query[R == 2 ? R * KD : 1][kWave];
     float(*meet)[16][LD] = reinterpret_cast<float(*)[16][LD]>(shared_u4);
     float2(*meet_ml)[16] = reinterpret_cast<float2(*)[16]>(reinterpret_cast<char *>(shared_u4) + kWaves * 16 * LD * 4);
 
@@ -241,7 +243,7 @@ __global__ __launch_bounds__(kWaves *kWave, D == 256 || R == 2 ? 2 : 4) void tre
     if (tile_1 < tiles) request(tile_1, 1, number_1);
 
     // query rows: channels (D / 4) q .. of this lane's row, in the order the nibbles come in
-    v8h qf[R][KD];
+    v8h qf[R == 2 ? 1 : KD];
     int new_row_of[R];
     uint64_t word[R];
     float bias[R];
@@ -258,10 +260,17 @@ __global__ __launch_bounds__(kWaves *kWave, D == 256 || R == 2 ? 2 : 4) void tre
             const v8h x = *reinterpret_cast<const v8h *>(src + 8 * d);
 #pragma unroll
             for (int e = 0; e < 8; ++e) sum += (float)x[e];
-            qf[r][d] = v8h{x[0], x[4], x[1], x[5], x[2], x[6], x[3], x[7]};
+            const v8h in_order = {x[0], x[4], x[1], x[5], x[2], x[6], x[3], x[7]};
+            if constexpr (R == 2) {
+                if (wave == (r * KD + d) % kWaves) query[r * KD + d][lane] = __builtin_bit_cast(uint4, in_order);
+            } else {
+                qf[d] = in_order;
+            }
         }
         bias[r] = -8.f * 0x1p-20f * quarter_sum(sum);
     }
+
+    if constexpr (R == 2) __syncthreads();
 
     while (tile < tiles) {
         // this tile has landed once only the requests behind it are outstanding
@@ -299,7 +308,8 @@ __global__ __launch_bounds__(kWaves *kWave, D == 256 || R == 2 ? 2 : 4) void tre
                 const uint32_t x = kx[f][d];
                 const v4i w = {(int)((x << 4) & 0x00F000F0u), (int)(x & 0x00F000F0u), (int)((x >> 4) & 0x00F000F0u), (int)((x >> 8) & 0x00F000F0u)};
 #pragma unroll
-                for (int r = 0; r < R; ++r) s[r][f] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(v8h, w), qf[r][d], s[r][f], 0, 0, 0);
+                for (int r = 0; r < R; ++r)
+                    s[r][f] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(v8h, w), R == 2 ? __builtin_bit_cast(v8h, query[r * KD + d][lane]) : qf[R == 2 ? 0 : d], s[r][f], 0, 0, 0);
             }
         // scores times steps (the mixed-precision multiply-add takes the fp16 as it is); keys that a row does not see
         float step_v[8];
@@ -325,22 +335,31 @@ __global__ __launch_bounds__(kWaves *kWave, D == 256 || R == 2 ? 2 : 4) void tre
                 }
             }
         }
-        float w[R][8], product[R][8];
-        bool large = false;
-        auto weigh = [&](int r) {
+        v8h p[R];
+        float sum[R];                                  // of the weights in fp32
+        auto weigh = [&](int r, bool held) {
+            float w[8];
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                w[r][e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r][e / 4][e % 4], a.score_scale, -M[r]));
-                product[r][e] = w[r][e] * step_v[e];
+                w[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r][e / 4][e % 4], a.score_scale, -M[r]));
+                if (held) w[e] = fminf(w[e], 0x1p14f * __builtin_amdgcn_rcpf(step_v[e]));
+                p[r][e] = (_Float16)(w[e] * step_v[e]);
             }
+            sum[r] = ((w[0] + w[1]) + (w[2] + w[3])) + ((w[4] + w[5]) + (w[6] + w[7]));
         };
+        v2h most = {0, 0};
 #pragma unroll
         for (int r = 0; r < R; ++r) {
-            weigh(r);
-            const float most = fmaxf(fmaxf(fmaxf(product[r][0], product[r][1]), fmaxf(product[r][2], product[r][3])),
-                                     fmaxf(fmaxf(product[r][4], product[r][5]), fmaxf(product[r][6], product[r][7])));
-            large = large | (most > 0x1p14f);
+            weigh(r, false);
+            const v4i pairs = __builtin_bit_cast(v4i, p[r]);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int pair = pairs[e];
+                most = __builtin_elementwise_max(most, __builtin_bit_cast(v2h, pair));
+            }
         }
+        const _Float16 most0 = most[0], most1 = most[1];
+        const bool large = (most0 > (_Float16)0x1p14f) | (most1 > (_Float16)0x1p14f);
         if (__any(large)) {
 #pragma unroll
             for (int r = 0; r < R; ++r) {
@@ -360,20 +379,12 @@ __global__ __launch_bounds__(kWaves *kWave, D == 256 || R == 2 ? 2 : 4) void tre
                 weights[r] *= fade;
 #pragma unroll
                 for (int j = 0; j < VT; ++j) o[r][j] *= fade;
-                weigh(r);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    w[r][e] = fminf(w[r][e], 0x1p14f * __builtin_amdgcn_rcpf(step_v[e]));
-                    product[r][e] = w[r][e] * step_v[e];
-                }
+                weigh(r, true);
             }
         }
-        v8h p[R];
 #pragma unroll
         for (int r = 0; r < R; ++r) {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) p[r][e] = (_Float16)product[r][e];
-            l[r] += ((w[r][0] + w[r][1]) + (w[r][2] + w[r][3])) + ((w[r][4] + w[r][5]) + (w[r][6] + w[r][7]));
+            l[r] += sum[r];
             weights[r] = __builtin_amdgcn_mfma_f32_16x16x32_f16(ones, p[r], weights[r], 0, 0, 0);
         }
         // values: unit lane % 16 of eight keys, two keys of one channel to a dword
