@@ -108,11 +108,11 @@ __device__ __forceinline__ int by_length(const CacheView &c, const AttentionCall
 // Softmax with a running offset M per row: a weight is exp2(s - M) times the value's step, rounded to fp16 (the normaliser
 // keeps the weight in fp32).  M stays as long as no product passes 2^14, which is seen when they are there (the maximum of
 // every tile took 7% more); then it goes by the row's largest sum of a score and the logarithm of the step.  That logarithm is
-// the step's fp32 bits taken as a number, at most 0.09 too small, so the largest product then is 2^7.9 to 2^7.99: just below
-// a power of two, where the steps of fp16 are the finest for it and its followers, and 21 octaves above the subnormals,
-// whatever the values' steps are.  (Outputs were 3.1e-4 off their exact values, in the 2-norm, with a first product of 2^0 or
-// 2^7, 2.7e-4 so; 2.1e-4 is the rounding of the output.  Two fp16 per weight give 2.1e-4 and take 139 us instead of 117 with
-// R = 1.)
+// the step's fp32 bits taken as a number, at most 0.09 too small, so the largest product then is 2^5.9 to 2^5.99: just below
+// a power of two, where the steps of fp16 are the finest for it and its followers, and 19 octaves above the subnormals,
+// whatever the values' steps are.  (16 trees / outputs' distance from their exact values in the 2-norm, where 2.1e-4 is the
+// rounding of the output: 2^7.9 83.5 us, 2.73e-4; 2^5.9 81.7, 2.81e-4; 2^1.9 79.8, 2.92e-4; 2^7 or 2^0 3.1e-4.  Two fp16 per
+// weight give 2.1e-4 and take 139 us instead of 117 with R = 1.)
 //
 // Loads: global memory -> LDS, two stages per wave; a tile goes to registers as soon as it has landed, and its stage is
 // requested again in front of the work on it, so two tiles are in flight all the time.  A wave waits for its own requests
@@ -373,7 +373,7 @@ __global__ __launch_bounds__(kWaves *kWave, D == 256 ? 2 : R == 2 ? 3 : 4) void 
                 // Where scores are huge their roundings count: M stays below the largest exponent by more than they are, so that
                 // key never vanishes, and products are held at 2^14.
                 top = __builtin_fmaf(fabsf(top), -0x1p-22f, top);
-                const float M_new = fmaxf(M[r], top - 7.9f), fade = __builtin_amdgcn_exp2f(M[r] - M_new);
+                const float M_new = fmaxf(M[r], top - 5.9f), fade = __builtin_amdgcn_exp2f(M[r] - M_new);
                 M[r] = M_new;
                 l[r] *= fade;
                 weights[r] *= fade;
