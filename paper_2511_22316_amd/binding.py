@@ -568,12 +568,19 @@ def sq_rotary_fp16(X, positions, turns, half, Y, magnitude=1.0, stream=None) -> 
     """Rotary positions on X fp16 [T, H, D] (any token and head strides) -> Y of the same shape (may be X).  positions
     int32 [T]; turns int64 [rot / 2] on the device, from sq_rotary_table; half: pairs (i, i + rot / 2), else (2i, 2i + 1)."""
     lib = _lib or _load()
-    T, H, D, ldx, ldh = _heads(X, "X", False)
-    ldy, ldyh = (ldx, ldh) if Y is X else _heads(Y, "Y", False)[3:]
+    shape = X.shape
+    if Y.shape != shape:
+        raise ValueError("Y must have the shape of X")
+    T, H, D = shape
+    ldx, ldh, one = X.stride()
+    ldy, ldyh, one_y = Y.stride()
+    if one != 1 or one_y != 1 or ldh < D or ldyh < D or H * ldh > ldx or H * ldyh > ldy or X.dtype is not _f16 or Y.dtype is not _f16:
+        ldx, ldh = _heads(X, "X", False)[3:]               # no usual layout: lengths of one, or a refusal
+        ldy, ldyh = _heads(Y, "Y", False)[3:]
     if positions.dtype is not _i32 or turns.dtype is not _i64 or not (positions.is_contiguous() and turns.is_contiguous()):
         _layout(("positions", positions, _i32, True), ("turns", turns, _i64, True))
-    if Y.shape != X.shape or positions.numel() != T:
-        raise ValueError("Y must have the shape of X, positions one entry per token")
+    if positions.numel() != T:
+        raise ValueError("positions must have one entry per token")
     code = lib.sq_rotary_fp16(X.data_ptr(), T, H, D, ldx, ldh, positions.data_ptr(), turns.data_ptr(), 2 * turns.numel(),
                               1 if half else 0, magnitude, Y.data_ptr(), ldy, ldyh, _here(stream, X, positions, turns, Y))
     if code:

@@ -928,3 +928,28 @@ def test_two_streams_at_once():
     for (_, out), want in zip(both, alone):
         assert all(torch.equal(a, b) for a, b in zip(out, want))
     assert not torch.equal(alone[0][2], alone[1][2])
+
+
+def test_rotary_lengths_of_one_with_any_stride():
+    import torch
+    import paper_2511_22316_amd as sq
+    g = rng(22)
+    turns, pos = sq.sq_rotary_table(32).cuda(), dev(np.arange(7, dtype=np.int32))
+    x = dev(rows(g, 7, 5 * 64).reshape(7, 5, 64))
+    want = torch.empty_like(x)
+    sq.sq_rotary_fp16(x, pos, turns, True, want)
+    y = torch.empty(1, 5, 64, dtype=torch.float16, device="cuda")
+    sq.sq_rotary_fp16(x[3:4].as_strided((1, 5, 64), (0, 64, 1), 3 * 320), pos[3:4].contiguous(), turns, True, y)
+    assert torch.equal(y, want[3:4])
+    y = torch.empty(7, 1, 64, dtype=torch.float16, device="cuda")
+    sq.sq_rotary_fp16(x.as_strided((7, 1, 64), (320, 1, 1), 2 * 64), pos, turns, True, y)
+    assert torch.equal(y, want[:, 2:3])
+    # rows whose last head ends where the next begins, and heads that overlap
+    gap = torch.zeros(7 * 5 * 72, dtype=torch.float16, device="cuda")
+    tight = gap.as_strided((7, 5, 64), (4 * 72 + 64, 72, 1))
+    tight.copy_(x)
+    out = torch.empty_like(want)
+    sq.sq_rotary_fp16(tight, pos, turns, True, out)
+    assert torch.equal(out, want)
+    with pytest.raises((ValueError, sq.SQError)):
+        sq.sq_rotary_fp16(x[:, :1].expand(7, 5, 64), pos, turns, True, want)
