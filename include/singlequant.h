@@ -445,9 +445,10 @@ sq_status sq_quantize_grouped(const void *X, int64_t T, int32_t K, int64_t ldx,
  * is legal and enqueues nothing.
  * At most 32 tokens: the sum of a group is exact products in fp32, then scaled in
  * fp32.  More tokens: code * step may be rounded to fp16 first (at most half a step of
- * fp16, and steps beyond 8188 may make it infinite), sums in fp32.  The order of the
- * additions goes with the sizes, and at most 32 tokens with the output channel's
- * number too.
+ * fp16; in a channel that has a step of 8192 or more, code * step / 8 is, so below the
+ * normal range off by up to 2^-22), sums in fp32; such a channel costs the walk over K
+ * once more.  The order of the additions goes with the sizes, and at most 32 tokens with
+ * the output channel's number too.
  */
 sq_status sq_w4a16_gemm_grouped(const void *X, int64_t T, int32_t K, int64_t ldx,
                                 const uint8_t *Qw, const void *steps, int32_t group, int32_t N,

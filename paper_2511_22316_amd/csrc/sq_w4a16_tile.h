@@ -60,9 +60,9 @@ __device__ __forceinline__ v8h widen_codes_f16(uint32_t w, uint32_t magic_vgpr)
 // instructions: the and-or is written as the one three-operand instruction it is (its
 // constants must come from registers in that form, which the compiler avoids by emitting two).
 template <int M>
-__device__ __forceinline__ uint32_t widen_byte_f16(uint32_t x, uint32_t magic_vgpr)
+__device__ __forceinline__ uint32_t widen_byte_f16(uint32_t x, uint32_t magic_vgpr, v2h scale = {(_Float16)1.f, (_Float16)0.0625f},
+                                                   v2h bias = {(_Float16)-1032.f, (_Float16)-72.f})
 {
-    const v2h scale = {(_Float16)1.f, (_Float16)0.0625f}, bias = {(_Float16)-1032.f, (_Float16)-72.f};
     const uint32_t sel = 0x0C000C00u | (uint32_t)M | ((uint32_t)M << 16);
     uint32_t h;
     asm("v_and_or_b32 %0, %1, %2, %3" : "=v"(h) : "v"(__builtin_amdgcn_perm(0u, x, sel)), "s"(0x00F0000Fu), "v"(magic_vgpr));
@@ -157,6 +157,9 @@ __device__ __forceinline__ void dma_step_if(const void *gptr, uint32_t lds_addr,
 // with a load per half T = 333, K = 5120, N = 13824, groups of 32 took 73.5 us, so 69.3), and a widened code is multiplied by its step in fp16, rounded once: a lane's 32
 // elements of a tile lie in one group, so that is one packed multiplication per two codes (four widening instructions
 // instead of three).  Scaling the sums instead would keep them exact, but wants as many registers again as the sums have.
+// Eight times a step from 8192 on is no fp16.  A wave notes the channels that have such steps on its way; where a workgroup has any it walks
+// over K once more (T = 2048, K = N = 4096: 75.7 us, 137 with such steps), those channels' codes taken by 1/8 and their sums by 8.  (Sums scaled in the middle of one walk: the
+// branch holds them twice, 60 registers more, and the large tiles spill.)
 template <int WM, int WN, int FM, int FN, int OCC, int BK, int LW, int KG, bool GROUPED>
 __global__ __launch_bounds__((KG * WM * WN + LW) * kWave, OCC) void w4a16_gemm_ring_kernel(
     const __half *__restrict__ X, int64_t ldx, int T, int K, const uint8_t *__restrict__ Qw,
@@ -195,122 +198,140 @@ __global__ __launch_bounds__((KG * WM * WN + LW) * kWave, OCC) void w4a16_gemm_r
         bm = group * GM + in_group % gm;
         bn = in_group / gm;
     }
-    const int row0 = bm * BM, col0 = bn * BN, Kb = K / 2;
+    const int Kb = K / 2;
     const int kg0 = kg * (K / KG);                               // this group's elements of K
-
-    // global -> LDS.  One wave-wide load fills 64 consecutive chunk slots: A_RPL rows of activations
-    // (lane l lands in row l / A_CPR, physical chunk l % A_CPR, which holds the logical chunk
-    // (l % A_CPR) ^ ((row / 2) % 8): sixteen consecutive rows, two per 256 bytes of the 64 banks, then
-    // keep the same logical chunk in sixteen different bank groups) or B_RPL rows of codes.  Rows past the ends are clamped: their
-    // products are never stored.
-    const __half *a_src[A_LOADS];
-    const uint8_t *b_src[B_LOADS];
-#pragma unroll
-    for (int u = 0; u < A_LOADS; ++u) {
-        const int r = A_RPL * (wave + NL * u) + lane / A_CPR;
-        a_src[u] = X + (int64_t)min(row0 + r, T - 1) * ldx + kg0 + (((lane % A_CPR) ^ ((r >> 1) & 7)) * 8);
-    }
-#pragma unroll
-    for (int u = 0; u < B_LOADS; ++u) {
-        const int r = B_RPL * (wave + NL * u) + lane / B_CPR;
-        b_src[u] = Qw + (int64_t)min(col0 + r, N - 1) * Kb + kg0 / 2 + (lane % B_CPR) * 16;
-    }
-    // steps: S_LANES channels per loading wave
-    const __half *s_src = nullptr;
-    if constexpr (GROUPED) s_src = sw + (int64_t)min(col0 + wave * S_LANES + lane % S_LANES, N - 1) * (K >> group_shift);
-    const uint32_t lds_base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint4 *)ring + kg * (NS * STAGE);
-    const uint32_t wave_u = __builtin_amdgcn_readfirstlane(wave);
-    auto issue_tile = [&](int kt, int stage, int limit) {
-        const uint32_t sa = lds_base + (uint32_t)stage * STAGE;
-#pragma unroll
-        for (int u = 0; u < A_LOADS; ++u) dma_16_if(a_src[u] + kt * BK, sa + (wave_u + NL * u) * 1024, kt, limit);
-#pragma unroll
-        for (int u = 0; u < B_LOADS; ++u)
-            dma_16_if(b_src[u] + kt * (BK / 2), sa + A_BYTES + (wave_u + NL * u) * 1024, kt, limit);
-        if constexpr (GROUPED)
-            dma_step_if<S_LANES>(s_src + ((kg0 + min(kt, limit - 1) * BK) >> group_shift), sa + A_BYTES + B_BYTES + wave_u * (4 * S_LANES), kt, limit,
-                                 group_shift);
-    };
-
+    int row0 = bm * BM, col0 = bn * BN;
     v16f acc[FM][FN];
-#pragma unroll
-    for (int i = 0; i < FM; ++i)
-#pragma unroll
-        for (int j = 0; j < FN; ++j)
-#pragma unroll
-            for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
+    uint32_t eighth[FN] = {};                          // channels of a fragment whose steps are taken by 1/8, a bit each
+    __shared__ uint32_t large_of[GROUPED ? KG : 1][GROUPED ? NW : 1][FN];
+#pragma unroll 1
+    for (int walk = 0; walk < (GROUPED ? 2 : 1); ++walk) {
+        if constexpr (GROUPED) asm volatile("" : "+s"(row0), "+s"(col0));      // what follows from them is found again, not kept from walk to walk
 
-    // LDS byte offsets of this lane's fragment chunks inside a stage: lane half g takes the elements
-    // [g BK / 2, (g + 1) BK / 2) of a K tile, step s the eight elements 8 s .. of those
-    int a_off[STEPS];
+        // global -> LDS.  One wave-wide load fills 64 consecutive chunk slots: A_RPL rows of activations
+        // (lane l lands in row l / A_CPR, physical chunk l % A_CPR, which holds the logical chunk
+        // (l % A_CPR) ^ ((row / 2) % 8): sixteen consecutive rows, two per 256 bytes of the 64 banks, then
+        // keep the same logical chunk in sixteen different bank groups) or B_RPL rows of codes.  Rows past the ends are clamped: their
+        // products are never stored.
+        const __half *a_src[A_LOADS];
+        const uint8_t *b_src[B_LOADS];
 #pragma unroll
-    for (int s = 0; s < STEPS; ++s)
-        a_off[s] = (wm * FM * 32 + l32) * A_ROW + (((STEPS * g + s) ^ ((l32 >> 1) & 7)) * 16);
-    const int b_off = A_BYTES + (wn * FN * 32 + l32) * B_ROW + g * (STEPS * 4);
-    const int s_off = A_BYTES + B_BYTES + (wn * FN * 32 + l32) * 4;
-    const uint32_t s_half = GROUPED && group_shift == 5 && g ? 0x03020302u : 0x01000100u;       // this lane's step of the dword, twice
-    const char *lds = reinterpret_cast<const char *>(ring) + kg * (NS * STAGE);
+        for (int u = 0; u < A_LOADS; ++u) {
+            const int r = A_RPL * (wave + NL * u) + lane / A_CPR;
+            a_src[u] = X + (int64_t)min(row0 + r, T - 1) * ldx + kg0 + (((lane % A_CPR) ^ ((r >> 1) & 7)) * 8);
+        }
+#pragma unroll
+        for (int u = 0; u < B_LOADS; ++u) {
+            const int r = B_RPL * (wave + NL * u) + lane / B_CPR;
+            b_src[u] = Qw + (int64_t)min(col0 + r, N - 1) * Kb + kg0 / 2 + (lane % B_CPR) * 16;
+        }
+        // steps: S_LANES channels per loading wave
+        const __half *s_src = nullptr;
+        if constexpr (GROUPED) s_src = sw + (int64_t)min(col0 + wave * S_LANES + lane % S_LANES, N - 1) * (K >> group_shift);
+        const uint32_t lds_base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint4 *)ring + kg * (NS * STAGE);
+        const uint32_t wave_u = __builtin_amdgcn_readfirstlane(wave);
+        auto issue_tile = [&](int kt, int stage, int limit) {
+            const uint32_t sa = lds_base + (uint32_t)stage * STAGE;
+#pragma unroll
+            for (int u = 0; u < A_LOADS; ++u) dma_16_if(a_src[u] + kt * BK, sa + (wave_u + NL * u) * 1024, kt, limit);
+#pragma unroll
+            for (int u = 0; u < B_LOADS; ++u)
+                dma_16_if(b_src[u] + kt * (BK / 2), sa + A_BYTES + (wave_u + NL * u) * 1024, kt, limit);
+            if constexpr (GROUPED)
+                dma_step_if<S_LANES>(s_src + ((kg0 + min(kt, limit - 1) * BK) >> group_shift), sa + A_BYTES + B_BYTES + wave_u * (4 * S_LANES), kt, limit,
+                                     group_shift);
+        };
 
-    uint32_t magic;                                    // 1024.0 in both halves, held in a vector register
-    asm volatile("v_mov_b32 %0, 0x64006400" : "=v"(magic));
-    const int ktiles = K / (KG * BK);
-    int stage = 0;
-    if (LW == 0 || loader) {
+        // LDS byte offsets of this lane's fragment chunks inside a stage: lane half g takes the elements
+        // [g BK / 2, (g + 1) BK / 2) of a K tile, step s the eight elements 8 s .. of those
+        int a_off[STEPS];
 #pragma unroll
-        for (int t = 0; t < NS - 1; ++t) issue_tile(t, t, ktiles);
-        wait_tile_and_barrier<LOADS, NS>(ktiles - 1);
-        issue_tile(NS - 1, NS - 1, ktiles);
-    } else {
-        asm volatile("s_barrier" ::: "memory");
-    }
-    if constexpr (LW > 0) {
-        if (loader) {
+        for (int s = 0; s < STEPS; ++s)
+            a_off[s] = (wm * FM * 32 + l32) * A_ROW + (((STEPS * g + s) ^ ((l32 >> 1) & 7)) * 16);
+        const int b_off = A_BYTES + (wn * FN * 32 + l32) * B_ROW + g * (STEPS * 4);
+        const int s_off = A_BYTES + B_BYTES + (wn * FN * 32 + l32) * 4;
+        const uint32_t s_half = GROUPED && group_shift == 5 && g ? 0x03020302u : 0x01000100u;       // this lane's step of the dword, twice
+        const char *lds = reinterpret_cast<const char *>(ring) + kg * (NS * STAGE);
+
+        uint32_t magic;                                    // 1024.0 in both halves, held in a vector register
+        asm volatile("v_mov_b32 %0, 0x64006400" : "=v"(magic));
+        const int ktiles = K / (KG * BK);
+#pragma unroll
+        for (int i = 0; i < FM; ++i)
+#pragma unroll
+            for (int j = 0; j < FN; ++j)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
+        int stage = 0;
+        if (LW == 0 || loader) {
+#pragma unroll
+            for (int t = 0; t < NS - 1; ++t) issue_tile(t, t, ktiles);
+            wait_tile_and_barrier<LOADS, NS>(ktiles - 1);
+            issue_tile(NS - 1, NS - 1, ktiles);
+        } else {
+            asm volatile("s_barrier" ::: "memory");
+        }
+        if (LW > 0 && loader) {
             // a loading wave: the waits and requests of the loop below and nothing else; it meets the
-            // multiplying waves at each of the 1 + ktiles barriers of the kernel
+            // multiplying waves at each of the 1 + ktiles barriers of the walk
             for (int kt = 0; kt < ktiles; ++kt) {
                 wait_tile_and_barrier<LOADS, NS>(ktiles - kt - 2);
                 issue_tile(kt + NS, stage, ktiles);
                 stage = stage == NS - 1 ? 0 : stage + 1;
             }
-            return;
-        }
-    }
+            if constexpr (!GROUPED) return;
+        } else {
 
-    // Operands run one step ahead of the MFMAs: while step s is multiplied, the activations of step s + 1 are read and its
-    // codes widened between the MFMAs, in the order written here.  A dword of codes per step: rb holds a tile's.
-    constexpr int NM = FM * FN;
-    static_assert(STEPS == 4 && NM >= 2, "four steps per tile");
-    typedef uint32_t v4u __attribute__((ext_vector_type(4)));
-    uint4 rb[FN];
-    v8h a[2][FM];
-    v4u b[2][FN];
-    uint32_t flipped[FN], step2[GROUPED ? FN : 1];     // step2: the step of this lane's half of the tile, twice
-    auto read_codes = [&](int stage_byte) {
+            // Operands run one step ahead of the MFMAs: while step s is multiplied, the activations of step s + 1 are read and its
+            // codes widened between the MFMAs, in the order written here.  A dword of codes per step: rb holds a tile's.
+            constexpr int NM = FM * FN;
+            static_assert(STEPS == 4 && NM >= 2, "four steps per tile");
+            typedef uint32_t v4u __attribute__((ext_vector_type(4)));
+            uint4 rb[FN];
+            v8h a[2][FM];
+            v4u b[2][FN];
+            uint32_t flipped[FN], step2[GROUPED ? FN : 1];     // step2: the step of this lane's half of the tile, twice
+            v2h scale[FN], bias[FN];                           // of the widening: codes, or codes / 8
+            _Float16 largest[GROUPED ? FN : 1];                // of the steps
+            if constexpr (GROUPED) {
 #pragma unroll
-        for (int j = 0; j < FN; ++j) rb[j] = *reinterpret_cast<const uint4 *>(lds + stage_byte + b_off + j * (32 * B_ROW));
-        if constexpr (GROUPED) {
+                for (int j = 0; j < FN; ++j) {
+                    const _Float16 share = (eighth[j] >> l32) & 1 ? (_Float16)0.125f : (_Float16)1.f;
+                    scale[j] = v2h{share, (_Float16)0.0625f * share};
+                    bias[j] = v2h{(_Float16)-1032.f * share, (_Float16)-72.f * share};
+                    largest[j] = 0;
+                }
+            }
+            auto read_codes = [&](int stage_byte) {
 #pragma unroll
-            for (int j = 0; j < FN; ++j) step2[j] = __builtin_amdgcn_perm(0u, *reinterpret_cast<const uint32_t *>(lds + stage_byte + s_off + j * (32 * 4)), s_half);
-        }
-    };
-    auto read_tokens = [&](int set, int stage_byte, int s, int i) {
-        a[set][i] = *reinterpret_cast<const v8h *>(lds + stage_byte + a_off[s] + i * (32 * A_ROW));
-    };
-    // unit u of 4 FN: byte u % 4 of the dword of step s of fragment u / 4
-    auto widen_unit = [&](int set, int s, int u) {
-        const int j = u / 4;
-        if (u % 4 == 0) flipped[j] = (s == 0 ? rb[j].x : s == 1 ? rb[j].y : s == 2 ? rb[j].z : rb[j].w) ^ 0x88888888u;
-        b[set][j][u % 4] = u % 4 == 0   ? widen_byte_f16<0>(flipped[j], magic)
-                           : u % 4 == 1 ? widen_byte_f16<1>(flipped[j], magic)
-                           : u % 4 == 2 ? widen_byte_f16<2>(flipped[j], magic)
-                                        : widen_byte_f16<3>(flipped[j], magic);
-        if constexpr (GROUPED) {
-            const uint32_t code2 = b[set][j][u % 4];
-            b[set][j][u % 4] = __builtin_bit_cast(uint32_t, __builtin_bit_cast(v2h, code2) * __builtin_bit_cast(v2h, step2[j]));
-        }
-    };
-    // One step on set C; the next one's operands are step S of the tile at BYTE.  TURN: the turn into that tile comes
-    // first, and its codes are read; they are widened in the second half of the step.
+                for (int j = 0; j < FN; ++j) rb[j] = *reinterpret_cast<const uint4 *>(lds + stage_byte + b_off + j * (32 * B_ROW));
+                if constexpr (GROUPED) {
+#pragma unroll
+                    for (int j = 0; j < FN; ++j) step2[j] = __builtin_amdgcn_perm(0u, *reinterpret_cast<const uint32_t *>(lds + stage_byte + s_off + j * (32 * 4)), s_half);
+                }
+            };
+            auto read_tokens = [&](int set, int stage_byte, int s, int i) {
+                a[set][i] = *reinterpret_cast<const v8h *>(lds + stage_byte + a_off[s] + i * (32 * A_ROW));
+            };
+            // unit u of 4 FN: byte u % 4 of the dword of step s of fragment u / 4
+            auto widen_unit = [&](int set, int s, int u) {
+                const int j = u / 4;
+                if (u % 4 == 0) flipped[j] = (s == 0 ? rb[j].x : s == 1 ? rb[j].y : s == 2 ? rb[j].z : rb[j].w) ^ 0x88888888u;
+                if constexpr (!GROUPED) {
+                    b[set][j][u % 4] = u % 4 == 0   ? widen_byte_f16<0>(flipped[j], magic)
+                                       : u % 4 == 1 ? widen_byte_f16<1>(flipped[j], magic)
+                                       : u % 4 == 2 ? widen_byte_f16<2>(flipped[j], magic)
+                                                    : widen_byte_f16<3>(flipped[j], magic);
+                } else {
+                    const uint32_t code2 = u % 4 == 0   ? widen_byte_f16<0>(flipped[j], magic, scale[j], bias[j])
+                                           : u % 4 == 1 ? widen_byte_f16<1>(flipped[j], magic, scale[j], bias[j])
+                                           : u % 4 == 2 ? widen_byte_f16<2>(flipped[j], magic, scale[j], bias[j])
+                                                        : widen_byte_f16<3>(flipped[j], magic, scale[j], bias[j]);
+                    b[set][j][u % 4] = __builtin_bit_cast(uint32_t, __builtin_bit_cast(v2h, code2) * __builtin_bit_cast(v2h, step2[j]));
+                }
+            };
+            // One step on set C; the next one's operands are step S of the tile at BYTE.  TURN: the turn into that tile comes
+            // first, and its codes are read; they are widened in the second half of the step.
 #define SQ_W16_STEP(C, BYTE, S, TURN)                                                                               \
     do {                                                                                                            \
         _Pragma("unroll") for (int m = 0; m < NM; ++m) {                                                            \
@@ -328,8 +349,8 @@ __global__ __launch_bounds__((KG * WM * WN + LW) * kWave, OCC) void w4a16_gemm_r
             __builtin_amdgcn_sched_barrier(0);                                                                      \
         }                                                                                                           \
     } while (0)
-    // Tile kt + 1 has landed once only the loads of the NS - 2 tiles behind it (those that exist) are outstanding.  Behind
-    // the barrier every wave's share of it is in LDS and all reads of tile kt are done, so its stage takes tile kt + NS.
+            // Tile kt + 1 has landed once only the loads of the NS - 2 tiles behind it (those that exist) are outstanding.  Behind
+            // the barrier every wave's share of it is in LDS and all reads of tile kt are done, so its stage takes tile kt + NS.
 #define SQ_W16_TURN()                                                                                               \
     do {                                                                                                            \
         if constexpr (LW == 0) {                                                                                    \
@@ -339,22 +360,52 @@ __global__ __launch_bounds__((KG * WM * WN + LW) * kWave, OCC) void w4a16_gemm_r
             asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");                                         \
         }                                                                                                           \
     } while (0)
-    read_codes(0);
+            read_codes(0);
 #pragma unroll
-    for (int i = 0; i < FM; ++i) read_tokens(0, 0, 0, i);
+            for (int i = 0; i < FM; ++i) read_tokens(0, 0, 0, i);
 #pragma unroll
-    for (int u = 0; u < 4 * FN; ++u) widen_unit(0, 0, u);
-    for (int kt = 0; kt < ktiles; ++kt) {
-        const int stage_n = stage == NS - 1 ? 0 : stage + 1;
-        const int cur_byte = stage * STAGE, next_byte = stage_n * STAGE;
-        SQ_W16_STEP(0, cur_byte, 1, 0);
-        SQ_W16_STEP(1, cur_byte, 2, 0);
-        SQ_W16_STEP(0, cur_byte, 3, 0);
-        SQ_W16_STEP(1, next_byte, 0, 1);          // behind the last tile: a stale stage, never used
-        stage = stage_n;
-    }
+            for (int u = 0; u < 4 * FN; ++u) widen_unit(0, 0, u);
+            for (int kt = 0; kt < ktiles; ++kt) {
+                const int stage_n = stage == NS - 1 ? 0 : stage + 1;
+                const int cur_byte = stage * STAGE, next_byte = stage_n * STAGE;
+                if constexpr (GROUPED) {
+#pragma unroll
+                    for (int j = 0; j < FN; ++j) largest[j] = __builtin_fmaxf16(largest[j], __builtin_fabsf16(__builtin_bit_cast(v2h, step2[j])[0]));
+                }
+                SQ_W16_STEP(0, cur_byte, 1, 0);
+                SQ_W16_STEP(1, cur_byte, 2, 0);
+                SQ_W16_STEP(0, cur_byte, 3, 0);
+                SQ_W16_STEP(1, next_byte, 0, 1);          // behind the last tile: a stale stage, never used
+                stage = stage_n;
+            }
 #undef SQ_W16_STEP
 #undef SQ_W16_TURN
+            if constexpr (GROUPED) {
+#pragma unroll
+                for (int j = 0; j < FN; ++j) {
+                    const uint64_t lanes = __ballot(largest[j] >= (_Float16)8192.f);       // both halves of the wave hold steps of the channel
+                    if (lane == 0) large_of[kg][wave][j] = (uint32_t)lanes | (uint32_t)(lanes >> 32);
+                }
+            }
+        }
+        if constexpr (GROUPED) {
+            if (walk == 1) break;
+            __syncthreads();                               // the flags are there, and all are done with the ring
+            uint32_t any = 0;
+#pragma unroll
+            for (int k = 0; k < KG; ++k)
+#pragma unroll
+                for (int w = 0; w < NW; ++w)
+#pragma unroll
+                    for (int j = 0; j < FN; ++j) any |= large_of[k][w][j];
+            if (__builtin_amdgcn_readfirstlane(any) == 0) break;
+#pragma unroll
+            for (int j = 0; j < FN; ++j)
+#pragma unroll
+                for (int k = 0; k < KG; ++k) eighth[j] = __builtin_amdgcn_readfirstlane(eighth[j] | large_of[k][wave][j]);
+        }
+    }
+    if (LW > 0 && loader) return;
 
     if constexpr (KG > 1) {
         constexpr int ACC = FM * FN * 16;
@@ -400,6 +451,11 @@ __global__ __launch_bounds__((KG * WM * WN + LW) * kWave, OCC) void w4a16_gemm_r
 #pragma unroll
         for (int i = 0; i < FM; ++i) {
             const int t = row0 + (wm * FM + i) * 32 + l32;
+            if (GROUPED && eighth[j]) {
+                const uint32_t mine = eighth[j] >> (4 * g);  // accumulator register e: channel 8 (e / 4) + 4 g + e % 4
+#pragma unroll
+                for (int e = 0; e < 16; ++e) acc[i][j][e] = (mine >> (8 * (e / 4) + e % 4)) & 1 ? 8.f * acc[i][j][e] : acc[i][j][e];
+            }
             uint32_t run[4][2];                              // run q: channels 8q + 4g .. + 3 as two dwords
 #pragma unroll
             for (int q = 0; q < 4; ++q)
