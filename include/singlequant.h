@@ -464,8 +464,9 @@ sq_status sq_w4a16_gemm_grouped(const void *X, int64_t T, int32_t K, int64_t ldx
  * first `rot` channels of a head; the others are copied as they are.
  *
  * sq_rotary_table   the frequencies, host only: turns[i] = f_i / (2 pi) in units of
- *              2^-64 of a turn, rounded to nearest.  A program may write a table of
- *              its own; the angle is then exact modulo a turn for any position.
+ *              2^-64 of a turn, to within a few of them (PARTS: a few times
+ *              high / (high - low)).  A program may write a table of its own; the angle
+ *              is exact modulo a turn, for what the table says, at any position.
  *              Plain: f_i = base^(-2i / rot).  For contexts `factor` times longer
  *              than the `trained` positions:
  *                SQ_ROTARY_LINEAR   f_i / factor

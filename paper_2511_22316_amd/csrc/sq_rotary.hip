@@ -3,6 +3,7 @@
 #include "sq_common.h"
 
 #include <cmath>
+#include <limits>
 
 namespace sq {
 
@@ -144,18 +145,25 @@ extern "C" sq_status sq_rotary_table(int32_t rot, double base, sq_rotary_scaling
     if (scaling == SQ_ROTARY_PARTS && (!(trained > 0.0) || !(low >= 0.0) || !(high > low) || !(high <= 1e18) || !(trained <= 1e18)))
         return SQ_ERR_SHAPE;
     if (!turns) return SQ_ERR_NULL;
-    const double two_pi = 6.283185307179586476925286766559;
-    if (scaling == SQ_ROTARY_BASE) base *= std::pow(factor, (double)rot / (double)(rot - 2));
+    // 64-bit significands: an entry is then right to a few of its units, and the angle of any 32-bit position to 2^-31 of a turn
+    // (in 64-bit numbers an entry is off by up to 2^9 and more, the farthest position's angle by more than the fp32 it ends in)
+    typedef long double wide;
+#ifndef __HIP_DEVICE_COMPILE__                         // the host's; the compiler's pass for the device takes it for 53
+    static_assert(std::numeric_limits<wide>::digits >= 64, "an entry has 62 bits");
+#endif
+    const wide two_pi = 6.283185307179586476925286766559005768L;
+    wide b = base;
+    if (scaling == SQ_ROTARY_BASE) b *= std::pow((wide)factor, (wide)rot / (wide)(rot - 2));
     for (int i = 0; i < rot / 2; ++i) {
-        double f = std::pow(base, -2.0 * i / rot);
+        wide f = std::pow(b, (wide)(-2 * i) / (wide)rot);
         if (scaling == SQ_ROTARY_LINEAR) f /= factor;
         if (scaling == SQ_ROTARY_PARTS) {
-            double keep = (trained * f / two_pi - low) / (high - low);
-            keep = keep < 0.0 ? 0.0 : keep > 1.0 ? 1.0 : keep;
-            f = f * keep + f / factor * (1.0 - keep);
+            wide keep = ((wide)trained * f / two_pi - low) / ((wide)high - low);
+            keep = keep < 0 ? 0 : keep > 1 ? 1 : keep;
+            f = f * keep + f / factor * (1 - keep);
         }
         // f <= 1 radian: below 2^62 in units of 2^-64 of a turn
-        turns[i] = (uint64_t)std::nearbyint(f / two_pi * 18446744073709551616.0);
+        turns[i] = (uint64_t)std::nearbyint(f / two_pi * 18446744073709551616.0L);
     }
     return SQ_OK;
 }

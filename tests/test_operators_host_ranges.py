@@ -1,0 +1,53 @@
+"""Host-side checks (no GPU) of the group, rotary, cache and attention calls at the ends of their ranges."""
+import decimal
+import os
+
+import numpy as np
+import pytest
+
+import paper_2511_22316_amd as sq
+from paper_2511_22316_amd import binding
+
+
+@pytest.fixture(scope="module")
+def lib():
+    if not os.path.exists(sq.library_path()):
+        from paper_2511_22316_amd import build
+        build.build()
+    return binding._load()
+
+
+def turns_exact(rot, base=10000.0, scaling=0, factor=1.0, trained=0.0, low=0.0, high=0.0):
+    """The frequencies in units of 2^-64 of a turn, to 60 digits."""
+    with decimal.localcontext() as c:
+        c.prec = 60
+        D = decimal.Decimal
+        two_pi = 2 * D("3.14159265358979323846264338327950288419716939937510582097494459")
+        base, factor, trained, low, high = (D(v) for v in (base, factor, trained, low, high))
+        if scaling == sq.SQ_ROTARY_BASE:
+            base *= (factor.ln() * rot / (rot - 2)).exp()
+        out = []
+        for i in range(rot // 2):
+            f = (base.ln() * (-2 * i) / rot).exp()
+            if scaling == sq.SQ_ROTARY_LINEAR:
+                f /= factor
+            if scaling == sq.SQ_ROTARY_PARTS:
+                keep = min(max((trained * f / two_pi - low) / (high - low), D(0)), D(1))
+                f = f * keep + f / factor * (1 - keep)
+            out.append(f / two_pi * 2 ** 64)
+        return out
+
+
+@pytest.mark.parametrize("rot", [2, 6, 128, 1024])
+@pytest.mark.parametrize("kind", [dict(), dict(base=500000.0), dict(base=1.0000001), dict(base=1e18), dict(scaling=sq.SQ_ROTARY_LINEAR, factor=3.0),
+                                  dict(scaling=sq.SQ_ROTARY_BASE, factor=2.7), dict(scaling=sq.SQ_ROTARY_BASE, factor=1e9),
+                                  dict(scaling=sq.SQ_ROTARY_PARTS, factor=8.0, trained=8192.0, low=1.0, high=32.0)])
+def test_rotary_table_to_the_last_units(lib, rot, kind):
+    """A frequency is a 64-bit fraction of a turn, and an angle is position * frequency modulo a turn: at position 2^31 an entry off by 2^10
+    units would be an angle off by 2^-23 of a turn.  The logarithm, power, quotients and sums are 64-bit significands: of a number below
+    2^61.4 units a few roundings are a few units."""
+    if rot == 2 and kind.get("scaling") == sq.SQ_ROTARY_BASE:
+        return
+    got = [int(v) for v in sq.sq_rotary_table(rot, **kind).numpy().view(np.uint64)]
+    off = [abs(g - w) for g, w in zip(got, turns_exact(rot, **kind))]
+    assert max(off) <= 4, (rot, kind, [int(o) for o in off[:8]])
