@@ -31,10 +31,13 @@ inline bool workgroup_per_row(int64_t T, int Hk, int D) { return T <= 1024 || Hk
 // their pieces of a line.  A launch for few rows is all latency (1 to 16 rows of 8 heads of 128: 3.1 us for either
 // kernel), many are bound by memory: 16384 rows of 8 heads of 128, 84 MB, 19.6 us in and 17.0 out (4.3 and 4.9 TB/s).
 template <int WAVES>
-__device__ __forceinline__ int64_t row_of_wave()
+__device__ __forceinline__ int64_t row_of_wave(int64_t T)
 {
-    const int64_t group = xcd_contiguous_id((int)blockIdx.x, (int)gridDim.x);
-    return group * (4 / WAVES) + __builtin_amdgcn_readfirstlane((int)(threadIdx.x / (WAVES * kWave)));
+    constexpr int ROWS = 4 / WAVES;                    // of a workgroup
+    const int64_t number = block_number();
+    const int groups = (int)((T + ROWS - 1) / ROWS);
+    if (number >= groups) return T;
+    return (int64_t)xcd_contiguous_id((int)number, groups) * ROWS + __builtin_amdgcn_readfirstlane((int)(threadIdx.x / (WAVES * kWave)));
 }
 
 template <int D, int WAVES>
@@ -43,7 +46,7 @@ __global__ __launch_bounds__(256) void cache_append_kernel(const CacheView c, co
 {
     constexpr int LANES = D / 8, AT_ONCE = 4 / WAVES, SHARE = WAVES * kWave;
     const int lane = (int)threadIdx.x % SHARE;
-    const int64_t row = row_of_wave<WAVES>();
+    const int64_t row = row_of_wave<WAVES>(T);
     if (row >= T) return;
     const int units = 2 * c.Hk * LANES;
     uint4 x[AT_ONCE];
@@ -99,7 +102,7 @@ __global__ __launch_bounds__(256) void cache_read_kernel(const CacheView c, __ha
 {
     constexpr int LANES = D / 8, AT_ONCE = 4 / WAVES, SHARE = WAVES * kWave;
     const int lane = (int)threadIdx.x % SHARE;
-    const int64_t row = row_of_wave<WAVES>();
+    const int64_t row = row_of_wave<WAVES>(T);
     if (row >= T) return;
     int slot;
     const uint8_t *page = place_of_row(c, row, slot);
@@ -180,7 +183,7 @@ extern "C" sq_status sq_cache_append(const void *K, int64_t ldk, const void *V, 
     const bool few = sq::workgroup_per_row(T, Hk, D);
     auto kernel = few ? (D == 64 ? sq::cache_append_kernel<64, 4> : D == 128 ? sq::cache_append_kernel<128, 4> : sq::cache_append_kernel<256, 4>)
                       : (D == 64 ? sq::cache_append_kernel<64, 1> : D == 128 ? sq::cache_append_kernel<128, 1> : sq::cache_append_kernel<256, 1>);
-    hipLaunchKernelGGL(kernel, dim3((unsigned)(few ? T : (T + 3) / 4)), dim3(256), 0, static_cast<hipStream_t>(stream), c,
+    hipLaunchKernelGGL(kernel, sq::grid_of(few ? T : (T + 3) / 4), dim3(256), 0, static_cast<hipStream_t>(stream), c,
                        static_cast<const __half *>(K), ldk, static_cast<const __half *>(V), ldv, T);
     return hipGetLastError() == hipSuccess ? SQ_OK : SQ_ERR_LAUNCH;
 }
@@ -195,7 +198,7 @@ extern "C" sq_status sq_cache_read(const void *cache, int32_t pages, int32_t Hk,
     const bool few = sq::workgroup_per_row(T, Hk, D);
     auto kernel = few ? (D == 64 ? sq::cache_read_kernel<64, 4> : D == 128 ? sq::cache_read_kernel<128, 4> : sq::cache_read_kernel<256, 4>)
                       : (D == 64 ? sq::cache_read_kernel<64, 1> : D == 128 ? sq::cache_read_kernel<128, 1> : sq::cache_read_kernel<256, 1>);
-    hipLaunchKernelGGL(kernel, dim3((unsigned)(few ? T : (T + 3) / 4)), dim3(256), 0, static_cast<hipStream_t>(stream), c, static_cast<__half *>(K),
+    hipLaunchKernelGGL(kernel, sq::grid_of(few ? T : (T + 3) / 4), dim3(256), 0, static_cast<hipStream_t>(stream), c, static_cast<__half *>(K),
                        ldk, static_cast<__half *>(V), ldv, T);
     return hipGetLastError() == hipSuccess ? SQ_OK : SQ_ERR_LAUNCH;
 }

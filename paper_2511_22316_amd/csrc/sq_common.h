@@ -46,6 +46,15 @@ __device__ __forceinline__ int xcd_contiguous_id(int wg, int nwg)
     return xcd * q + (xcd < r ? xcd : r) + local;
 }
 
+// A launch counts its threads along x in 32 bits: workgroups (of 256 threads) beyond kGridRow go on along y.  The last row has
+// workgroups too many, which block_number() tells.
+constexpr int64_t kGridRow = 1 << 23, kMaxBlocks = kGridRow * 65535;
+inline dim3 grid_of(int64_t blocks)
+{
+    return blocks <= kGridRow ? dim3((unsigned)blocks) : dim3((unsigned)kGridRow, (unsigned)((blocks + kGridRow - 1) / kGridRow));
+}
+__device__ __forceinline__ int64_t block_number() { return (int64_t)blockIdx.y * gridDim.x + blockIdx.x; }
+
 // Maximum of a non-negative value over the 64 lanes, returned in every lane.  Cross-lane steps
 // use DPP modifiers (register-file speed) rather than LDS permutes.
 __device__ __forceinline__ float wave_max(float v)

@@ -56,7 +56,7 @@ extern "C" sq_status sq_quantize_grouped(const void *X, int64_t T, int32_t K, in
 {
     if (group != 32 && group != 64 && group != 128 && group != 256) return SQ_ERR_SHAPE;
     if (T < 0 || T > SQ_MAX_ROWS || K <= 0 || K > 131072 || (K % group) != 0 || ldx < K) return SQ_ERR_SHAPE;
-    if (T * (int64_t)(K / 8) > (int64_t)1024 * 0x7FFFFFFF) return SQ_ERR_SHAPE;      // blocks of a launch
+    if (T * (int64_t)(K / 8) >= (int64_t)1024 << 24) return SQ_ERR_SHAPE;       // a launch counts 2^32 threads; so much of X fills the device
     if (T == 0) return SQ_OK;
     if (!X || !Q || !steps) return SQ_ERR_NULL;
     if (((uintptr_t)X & 15) || (ldx % 8) != 0 || ((uintptr_t)Q & 15) || ((uintptr_t)steps & 1)) return SQ_ERR_ALIGN;

@@ -44,7 +44,7 @@ __global__ __launch_bounds__(256) void rotary_kernel(const __half *X, int64_t T,
                                                      int slots)
 {
     typedef _Float16 Halves __attribute__((ext_vector_type(V)));
-    const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    const int64_t id = block_number() * 256 + threadIdx.x;
     const int per_token = units * slots;
     const int64_t t = id / per_token;
     if (t >= T) return;
@@ -92,7 +92,7 @@ __global__ __launch_bounds__(256) void rotary_pair_kernel(const __half *X, int64
                                                           const uint64_t *__restrict__ turns, int rot, int half,
                                                           float magnitude, __half *Y, int64_t ldy, int64_t ldyh, int units)
 {
-    const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    const int64_t id = block_number() * 256 + threadIdx.x;
     const int64_t row = id / units, t = row / H;
     if (t >= T) return;
     const int u = (int)(id - row * units), h = (int)(row - t * H);
@@ -121,10 +121,10 @@ sq_status launch_rotary(const __half *x, int64_t T, int H, int D, int64_t ldx, i
     if (want < 8) want = 8;
     const int slots = (int)(want < H ? want : H);
     const int64_t blocks = (lanes * slots + 255) / 256;
-    if (blocks > 0x7FFFFFFF) return SQ_ERR_SHAPE;
+    if (blocks > kMaxBlocks) return SQ_ERR_SHAPE;
     auto kernel = half ? (copied ? rotary_kernel<V, true, true> : rotary_kernel<V, true, false>)
                        : (copied ? rotary_kernel<V, false, true> : rotary_kernel<V, false, false>);
-    hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(256), 0, st, x, T, H, D, ldx, ldh, positions, turns, rot, magnitude, y, ldy, ldyh, units,
+    hipLaunchKernelGGL(kernel, grid_of(blocks), dim3(256), 0, st, x, T, H, D, ldx, ldh, positions, turns, rot, magnitude, y, ldy, ldyh, units,
                        slots);
     return hipGetLastError() == hipSuccess ? SQ_OK : SQ_ERR_LAUNCH;
 }
@@ -197,8 +197,8 @@ extern "C" sq_status sq_rotary_fp16(const void *X, int64_t T, int32_t H, int32_t
     if (places(2)) return sq::launch_rotary<2>(x, T, H, D, ldx, ldh, positions, turns, rot, half, magnitude, y, ldy, ldyh, copied, st);
     const int units = rot / 2 + copied;
     const int64_t blocks = (T * H * units + 255) / 256;
-    if (blocks > 0x7FFFFFFF) return SQ_ERR_SHAPE;
-    hipLaunchKernelGGL(sq::rotary_pair_kernel, dim3((unsigned)blocks), dim3(256), 0, st, x, T, H, D, ldx, ldh, positions, turns, rot, half,
+    if (blocks > sq::kMaxBlocks) return SQ_ERR_SHAPE;
+    hipLaunchKernelGGL(sq::rotary_pair_kernel, sq::grid_of(blocks), dim3(256), 0, st, x, T, H, D, ldx, ldh, positions, turns, rot, half,
                        magnitude, y, ldy, ldyh, units);
     return hipGetLastError() == hipSuccess ? SQ_OK : SQ_ERR_LAUNCH;
 }

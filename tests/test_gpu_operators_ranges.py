@@ -55,3 +55,58 @@ def test_product_of_steps_that_are_not_finite():
         there = np.isin(np.arange(N), (7, 70))
         assert not np.isfinite(got[:, there]).any()
         ou.held(got[:, ~there], want[:, ~there], bound[:, ~there], f"{T} {N}")
+
+
+# ---- more threads than a launch counts along x -------------------------------------------------------
+
+
+def test_rotary_of_more_pairs_than_32_bits():
+    """2^32 pairs and a token more, in a place that allows one pair per lane, against the same tokens by themselves."""
+    import torch
+    import paper_2511_22316_amd as sq
+    print("case rotary 2^32 pairs", flush=True)
+    T, H, D = (1 << 22) + 1, 1024, 2
+    base = dev(rows(rng(40), 1, H * D))[0]
+    buf = torch.empty(1 + T * H * D, dtype=torch.float16, device="cuda")
+    x = buf[1:].view(T, H, D)
+    x[:] = base.view(H, D)
+    pos = torch.arange(T, dtype=torch.int32, device="cuda")
+    turns = sq.sq_rotary_table(D, base=3.0).cuda()
+    sq.sq_rotary_fp16(x, pos, turns, False, x)
+    for first in (0, (1 << 21) - 5, T - 300):
+        few = base.view(1, H, D).repeat(300, 1, 1)
+        sq.sq_rotary_fp16(few, pos[first: first + 300].contiguous(), turns, False, few)
+        assert torch.equal(x[first: first + 300], few), first
+    del buf, x
+    torch.cuda.empty_cache()
+
+
+def test_cache_of_more_rows_than_a_row_of_workgroups():
+    import torch
+    import paper_2511_22316_amd as sq
+    print("case cache 2^26 rows", flush=True)
+    T, D, page, n = (1 << 26) + 5, 64, 1024, 1 << 16
+    base = dev(rows(rng(41), n, D))
+    few = [torch.empty(n, 1, D, dtype=torch.float16, device="cuda") for _ in range(2)]
+    i32 = lambda *v: torch.tensor(v, dtype=torch.int32, device="cuda")       # noqa: E731
+    pages = -(-T // page)
+    cache = torch.empty(pages, sq.sq_cache_page_bytes(1, D, page), dtype=torch.uint8, device="cuda")
+    table = torch.arange(pages, dtype=torch.int32, device="cuda")[None].contiguous()
+    k, v = base.view(n, 1, D), base.flip(0).view(n, 1, D).contiguous()
+    sq.sq_cache_append(k, v, i32(0, n), i32(0), table, page, cache)
+    sq.sq_cache_read(cache, i32(0, n), i32(0), table, page, *few)
+    cache.zero_()
+    many = [torch.empty(T, 1, D, dtype=torch.float16, device="cuda") for _ in range(2)]
+    for t, x in zip(many, (k, v)):
+        t[: T - 5].view(-1, n, D)[:] = x.view(1, n, D)
+        t[T - 5:] = x[:5]
+    sq.sq_cache_append(*many, i32(0, T), i32(0), table, page, cache)
+    for t in many:
+        t.fill_(3.0)
+    sq.sq_cache_read(cache, i32(0, T), i32(0), table, page, *many)
+    for t, x in zip(many, few):
+        assert torch.equal(t[T - 5:], x[:5])
+        for part in t[: T - 5].view(-1, n, 1, D):
+            assert torch.equal(part, x)
+    del many, cache
+    torch.cuda.empty_cache()
