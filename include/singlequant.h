@@ -441,8 +441,8 @@ sq_status sq_quantize_grouped(const void *X, int64_t T, int32_t K, int64_t ldx,
  *   steps    device, fp16 [N, K / group], group 32, 64, 128 or 256; 4-byte aligned
  *            with groups of 32
  *   Y        device out, fp16 [T, ldy], ldy >= N
- * Requires K % 64 == 0, K % group == 0, K <= 131072, T <= 2^24.  T == 0 or N == 0
- * is legal and enqueues nothing.
+ * Requires K % 64 == 0, K % group == 0, K <= 131072, T <= 2^24, N <= 2^28.  T == 0 or
+ * N == 0 is legal and enqueues nothing.
  * At most 32 tokens: the sum of a group is exact products in fp32, then scaled in
  * fp32.  More tokens: code * step may be rounded to fp16 first (at most half a step of
  * fp16; in a channel that has a step of 8192 or more, code * step / 8 is, so below the

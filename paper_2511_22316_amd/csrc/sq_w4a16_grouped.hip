@@ -646,7 +646,7 @@ extern "C" sq_status sq_w4a16_gemm_grouped(const void *X, int64_t T, int32_t K, 
 {
     if (group != 32 && group != 64 && group != 128 && group != 256) return SQ_ERR_SHAPE;
     if (T < 0 || N < 0 || K <= 0 || (K % 64) != 0 || (K % group) != 0 || K > 131072) return SQ_ERR_SHAPE;
-    if (T > (1 << 24) || ldx < K || ldy < N) return SQ_ERR_SHAPE;
+    if (T > (1 << 24) || N > (1 << 28) || ldx < K || ldy < N) return SQ_ERR_SHAPE;      // 2^28 channels: their numbers, padded, and the grids stay in 32 bits
     if (T == 0 || N == 0) return SQ_OK;
     if (!X || !Qw || !steps || !Y) return SQ_ERR_NULL;
     if (((uintptr_t)X & 15) || (ldx % 8) != 0 || ((uintptr_t)Qw & 15) || ((uintptr_t)Y & 1) || ((uintptr_t)steps & (group == 32 ? 3 : 1)))

@@ -498,8 +498,9 @@ sq_status launch_w4a16_ring(const __half *X, int64_t ldx, int T, int K, const ui
     static_assert(lds <= (size_t)kMaxDynamicLds, "ring does not fit in LDS");
     auto kernel = w4a16_gemm_ring_kernel<WM, WN, FM, FN, OCC, BK, LW, KG, GROUPED>;
     if ((K % (KG * BK)) != 0) return SQ_ERR_SHAPE;
+    const int tiles_m = (T + BM - 1) / BM, tiles_n = (int)(((int64_t)N + BN - 1) / BN);
+    if ((int64_t)tiles_m * tiles_n * ((KG * WM * WN + LW) * kWave) > 0xFFFFFFFFll) return SQ_ERR_SHAPE;       // threads of a launch
     if (!allow_large_lds(reinterpret_cast<const void *>(kernel))) return SQ_ERR_LAUNCH;
-    const int tiles_m = (T + BM - 1) / BM, tiles_n = (N + BN - 1) / BN;
     const int vec_store = (((uintptr_t)Y & 15) == 0 && (ldy % 8) == 0) ? 1 : 0;
     hipLaunchKernelGGL(kernel, dim3((unsigned)(tiles_m * tiles_n)), dim3((KG * WM * WN + LW) * kWave), lds, st, X, ldx, T, K, Qw,
                        sw, N, Y, ldy, tiles_m, tiles_n, vec_store, group_shift);

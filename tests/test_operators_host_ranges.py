@@ -51,3 +51,13 @@ def test_rotary_table_to_the_last_units(lib, rot, kind):
     got = [int(v) for v in sq.sq_rotary_table(rot, **kind).numpy().view(np.uint64)]
     off = [abs(g - w) for g, w in zip(got, turns_exact(rot, **kind))]
     assert max(off) <= 4, (rot, kind, [int(o) for o in off[:8]])
+
+
+def test_grouped_product_refuses_more_channels_than_it_numbers(lib):
+    """Channel numbers are 32-bit and are padded to a tile's end."""
+    FAKE, SHAPE = 0x1000, 2                                 # never dereferenced: validation fails first
+    for T in (1, 16, 32, 33, 64, 1000):
+        for N in ((1 << 28) + 1, 2 ** 31 - 1):
+            for group in (32, 256):
+                assert lib.sq_w4a16_gemm_grouped(FAKE, T, 256, 256, FAKE, FAKE, group, N, FAKE, N, None) == SHAPE, (T, N, group)
+    assert lib.sq_w4a16_gemm_grouped(FAKE, 1 << 24, 256, 256, FAKE, FAKE, 64, 1 << 28, FAKE, 1 << 28, None) == SHAPE     # 2^37 tiles
