@@ -574,7 +574,9 @@ sq_status sq_cache_read(const void *cache, int32_t pages, int32_t Hk, int32_t D,
  *   mask       device, uint64 [T], or NULL.  With a mask a sequence has at most 64 new
  *              rows (further ones are not seen by any).
  *   max_rows   at least the new rows of every sequence (those from max_rows on are left
- *              out: their rows of O keep what they held); <= 64 with a mask
+ *              out: their rows of O keep what they held); <= 64 with a mask.  Work is
+ *              shared out for the T rows there are; all sequences are split alike, so
+ *              few rows over many keys are best not in one call with a long prompt.
  *   max_keys   about the longest cached[b] + new rows: how finely the work is split.
  *              Any value gives the right result.
  *   scale      in (0, 1e20); scores scale * Q . k beyond 2^24 are not told apart

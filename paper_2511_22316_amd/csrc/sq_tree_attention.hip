@@ -56,7 +56,9 @@ struct AttentionCall {
     const uint64_t *mask;
     float *part;               // [T, Hq, splits, D] sums of a split, then [T, Hq, splits] (maximum, sum); null: one split
     int64_t ldq, ldo, T;
-    int Hq, group, max_rows, splits, row_blocks, tiles_per_chunk;
+    int Hq, group, max_rows, splits, tiles_per_chunk;
+    int row_blocks;            // of 16 R rows: of every sequence, or of all of them (packed)
+    int blocks;                // workgroups of the first launch
     float score_scale;         // scale * log2(e) * 2^20
 };
 
@@ -83,6 +85,34 @@ __device__ __forceinline__ int by_length(const CacheView &c, const AttentionCall
     int longer = lane < c.B ? 0 : kWave;
     for (int i = 0; i < c.B; ++i) longer += (uint32_t)__builtin_amdgcn_readlane((int)key, i) > key ? 1 : 0;
     return __builtin_ctzll(__ballot(longer == place));
+}
+
+// Packed row blocks: where some sequences have many rows and most have few, row blocks for the longest in every sequence would be
+// workgroups without rows nearly all of them.  Sequence b's blocks are then numbered from f(b) = floor(start group / 16 R) + b on, start
+// being its first row: f grows by one at least, and by as many as its rows need, and the last number is below
+// floor(T group / 16 R) + B.  The sequence of block `number` (the last b with f(b) <= number; -1: none), and which of its blocks that is;
+// 64 probes at a time, as owner_of_row.
+template <int R>
+__device__ __forceinline__ int sequence_of_block(const CacheView &c, const AttentionCall &a, int number, int &block)
+{
+    const int lane = (int)(threadIdx.x & (kWave - 1));
+    auto first_block = [&](int b) { return (int)(min(max((int64_t)c.row_start[b], (int64_t)0), a.T) * a.group / (16 * R)) + b; };
+    int lo = 0, count = c.B;
+    while (true) {
+        const int step = (count + kWave - 1) / kWave, at = lo + lane * step;
+        int f = 0;
+        const bool there = at < lo + count;
+        if (there) f = first_block(at);
+        const int hits = __popcll(__ballot(there && f <= number));
+        if (hits == 0) return -1;
+        if (step == 1) {
+            block = number - __builtin_amdgcn_readlane(f, hits - 1);
+            return lo + hits - 1;
+        }
+        const int next = lo + (hits - 1) * step;
+        count = min(step, lo + count - next);
+        lo = next;
+    }
 }
 
 // A workgroup takes one head of K and V of one sequence, 16 R query rows (row = new row * group + query head in the group)
@@ -117,8 +147,9 @@ __device__ __forceinline__ int by_length(const CacheView &c, const AttentionCall
 // Loads: global memory -> LDS, two stages per wave; a tile goes to registers as soon as it has landed, and its stage is
 // requested again in front of the work on it, so two tiles are in flight all the time.  A wave waits for its own requests
 // only.  The page numbers are requested a tile ahead of that.
-// ONE_PAGE: pages of 32 rows and more, a tile lies in one.
-template <int D, bool ONE_PAGE, int R>
+// ONE_PAGE: pages of 32 rows and more, a tile lies in one.  PACKED: row blocks numbered as above (an instantiation of its own: the test
+// alone took 0.1 to 0.4 us of a launch for one token).
+template <int D, bool ONE_PAGE, int R, bool PACKED>
 __global__ __launch_bounds__(kWaves *kWave, D == 256 ? 2 : R == 2 ? 3 : 4) void tree_attention_kernel(const CacheView c, const AttentionCall a)
 {
     constexpr int KD = D / 32;                       // dwords of K (and of V) per lane and 16 keys; steps of the scores
@@ -133,13 +164,22 @@ __global__ __launch_bounds__(kWaves *kWave, D == 256 ? 2 : R == 2 ? 3 : 4) void 
 
     const int lane = threadIdx.x & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
     const int l16 = lane & 15, q = lane >> 4;
-    int id = xcd_contiguous_id((int)blockIdx.x, (int)gridDim.x);
+    if (PACKED && block_number() >= a.blocks) return;
+    int id = PACKED ? xcd_contiguous_id((int)block_number(), a.blocks) : xcd_contiguous_id((int)blockIdx.x, (int)gridDim.x);
     // of a prompt's rows the last ones see the most: they start first (4096 rows 221 -> 214 us; of a tree all see about the same)
-    const int row_block = a.mask ? id % a.row_blocks : a.row_blocks - 1 - id % a.row_blocks;
+    int row_block = a.mask ? id % a.row_blocks : a.row_blocks - 1 - id % a.row_blocks;
     id /= a.row_blocks;
     const int split = id % a.splits;
     id /= a.splits;
-    const int h = id / c.B, b = R == 1 ? id % c.B : by_length(c, a, id % c.B);
+    int h, b;
+    if constexpr (PACKED) {
+        h = id;
+        b = sequence_of_block<R>(c, a, row_block, row_block);
+        if (b < 0) return;
+    } else {
+        h = id / c.B;
+        b = R == 1 ? id % c.B : by_length(c, a, id % c.B);
+    }
 
     uint32_t chunk_end = (uint32_t)(split + 1) * a.tiles_per_chunk;
     const uint32_t to_next_chunk = (uint32_t)(a.splits - 1) * a.tiles_per_chunk;
@@ -477,17 +517,24 @@ __global__ __launch_bounds__(kWaves *kWave, D == 256 ? 2 : R == 2 ? 3 : 4) void 
 
 // The splits of a row and head, at most kMaxSplits: one workgroup, D / 4 threads to a split, so that all sums are requested at
 // once.  (One wave walking over the splits took 17.7 us for 64 of them.)
-template <int D>
+template <int D, bool PACKED>
 __global__ __launch_bounds__(256) void tree_attention_join_kernel(const CacheView c, const AttentionCall a)
 {
     constexpr int LANES = D / 4, SIDE = 256 / LANES, MOST = kMaxSplits / SIDE;     // threads of a split; splits side by side; rounds of them
     __shared__ float shares[kMaxSplits], totals;
     __shared__ float4 sums[SIDE][LANES];
     const int tid = threadIdx.x, lane = tid & (kWave - 1), mine = tid % LANES, side = tid / LANES;
-    const int b = blockIdx.y, i = (int)(blockIdx.x / (unsigned)a.Hq), hq = (int)(blockIdx.x % (unsigned)a.Hq);
+    int i = (int)(blockIdx.x / (unsigned)a.Hq), hq = (int)(blockIdx.x % (unsigned)a.Hq);       // new row of sequence blockIdx.y, or (PACKED) of the call
     int64_t first;
-    const int n = rows_of(c, a, b, first);
-    if (i >= min(n, a.max_rows)) return;
+    if constexpr (PACKED) {
+        const RowOwner r = owner_of_row(c, i);
+        first = r.first;
+        if (r.b < 0 || first < 0 || i - first >= a.max_rows) return;
+        i -= (int)first;
+    } else {
+        const int n = rows_of(c, a, (int)blockIdx.y, first);
+        if (i >= min(n, a.max_rows)) return;
+    }
     const int64_t place = ((first + i) * a.Hq + hq) * a.splits;
     const float2 ml = reinterpret_cast<const float2 *>(a.part + a.T * a.Hq * (int64_t)a.splits * D)[place + min(lane, a.splits - 1)];
     float4 v[MOST];
@@ -530,17 +577,15 @@ __global__ __launch_bounds__(256) void tree_attention_join_kernel(const CacheVie
     *reinterpret_cast<v4hs *>(a.O + (first + i) * a.ldo + hq * D + 4 * mine) = y;
 }
 
-template <int D, bool ONE_PAGE, int R>
+template <int D, bool ONE_PAGE, int R, bool PACKED>
 sq_status launch_tree_attention(const CacheView &c, const AttentionCall &a, hipStream_t st)
 {
-    const int64_t blocks = (int64_t)a.row_blocks * a.splits * c.Hk * c.B;
-    if (blocks > 0x7FFFFFFF) return SQ_ERR_SHAPE;
-    hipLaunchKernelGGL((tree_attention_kernel<D, ONE_PAGE, R>), dim3((unsigned)blocks), dim3(kWaves * kWave), 0, st, c, a);
+    hipLaunchKernelGGL((tree_attention_kernel<D, ONE_PAGE, R, PACKED>), grid_of(a.blocks), dim3(kWaves * kWave), 0, st, c, a);
     if (hipGetLastError() != hipSuccess) return SQ_ERR_LAUNCH;
     if (a.splits == 1) return SQ_OK;
-    const int64_t units = (int64_t)a.max_rows * a.Hq;
-    if (units > 0x7FFFFFFF) return SQ_ERR_SHAPE;
-    hipLaunchKernelGGL(tree_attention_join_kernel<D>, dim3((unsigned)units, (unsigned)c.B), dim3(256), 0, st, c, a);
+    // few: what is split has at most 512 workgroups in all, of 32 rows
+    const unsigned rows = (unsigned)((PACKED ? a.T : a.max_rows) * a.Hq);
+    hipLaunchKernelGGL((tree_attention_join_kernel<D, PACKED>), dim3(rows, PACKED ? 1u : (unsigned)c.B), dim3(256), 0, st, c, a);
     return hipGetLastError() == hipSuccess ? SQ_OK : SQ_ERR_LAUNCH;
 }
 
@@ -551,19 +596,25 @@ sq_status dispatch_tree_attention(const CacheView &c, AttentionCall &a, int64_t 
     const int64_t rows = (int64_t)a.max_rows * a.group;
     if (rows > (1 << 30)) return SQ_ERR_SHAPE;
     max_keys = max_keys < 1 ? 1 : max_keys;
+    // Row blocks of all sequences: as many as the longest has in each, or packed, where that is less than half (or those are more than
+    // one row of a grid).  Us, even / packed, a prompt among sequences of one row (32 heads of 128, 8 of K and V): 2048 rows, 63 others of 2048
+    // keys 660 / 91, of 32768 1876 / 612; 64 rows, 32 of 1024 44 / 15; 300 rows, 999 of 300 541 / 130.
+    auto even = [&](int64_t per_block) { return (rows + per_block - 1) / per_block * c.B; };
+    auto packed = [&](int64_t per_block) { return a.T * a.group / per_block + c.B; };
+    auto pack = [&](int64_t per_block) { return 2 * packed(per_block) < even(per_block) || even(per_block) * c.Hk > kGridRow; };
+    auto row_blocks = [&](int64_t per_block) { return pack(per_block) ? packed(per_block) : even(per_block); };
     // 32 rows per workgroup from about two waves of work for every SIMD on (us, 16 / 32: 16 sequences, 20 rows, 1024 keys 16.8 /
     // 18.6; one prompt of 300 rows 13.2 / 15.3; 16 sequences, 32 rows, 4096 keys 30.5 / 30.7; one tree of 61 new rows, 16384 keys
     // 44.7 / 39.9; 64 sequences, 28 rows, 8192 keys 122.7 / 103.2).  256 channels of two tiles of rows do not fit in registers.
-    const int64_t blocks_of_16 = (rows + 15) / 16 * c.Hk * c.B;
-    const int64_t per_block = D < 256 && rows > 16 && (double)blocks_of_16 * (double)max_keys > 0x1p20 ? 32 : 16;
-    a.row_blocks = (int)((rows + per_block - 1) / per_block);
+    const int64_t per_block = D < 256 && rows > 16 && (double)(row_blocks(16) * c.Hk) * (double)max_keys > 0x1p20 ? 32 : 16;
+    const bool is_packed = pack(per_block);
     // Splits of the keys: as many as give every CU a workgroup, twice (four times, of many units) that while a split has 2048 keys
     // or more, no more than there are chunks of 128 keys, and none where the keys' tiles take less time than the second launch,
     // about 3 us (us without a split / best / 1024 workgroups, one row of 32 heads per sequence, 8 of K and V, D = 128: one sequence
     // of 512 keys 6.9 / 7.7 / 7.7, of 1024 9.5 / 7.8 / 7.8, of 16384 92 / 11.7 / 13.0; 4 of 4096 26.7 / 11.6 with 8 / 13.5, of 16384
     // 93 / 19.0 with 16 / 20.8; 16 of 1024 10.5 / 11.8 with 2 / 13.3, of 4096 26.9 / 19.5 with 4 / 21.3; 48 of 4096 to 8192 74.2 / 70.6
     // with 2).  And no more than the workspace holds.
-    const int64_t units = (int64_t)a.row_blocks * c.Hk * c.B, most = units > 256 && per_block == 16 ? 1024 : 512;
+    const int64_t units = row_blocks(per_block) * c.Hk, most = units > 256 && per_block == 16 ? 1024 : 512;
     const int64_t chunks = (max_keys + kChunkUnit - 1) / kChunkUnit, room = workspace_bytes / (a.T * a.Hq * (D + 2) * 4);
     int64_t splits = units < 256 ? 256 / units : 1;
     while (2 * splits * units <= most && max_keys >= 2048 * splits) splits *= 2;
@@ -572,11 +623,19 @@ sq_status dispatch_tree_attention(const CacheView &c, AttentionCall &a, int64_t 
     if (max_keys * (splits - 1) < 590 * splits) splits = 1;
     splits = splits < room ? splits : room;
     a.splits = splits < 1 ? 1 : (int)splits;
+    if (units * a.splits > 0x7FFFFFFF) return SQ_ERR_SHAPE;
+    a.blocks = (int)(units * a.splits);
+    a.row_blocks = (int)(is_packed ? packed(per_block) : even(per_block) / c.B);
     a.part = static_cast<float *>(workspace);
     a.tiles_per_chunk = kWaves * (int)((chunks + a.splits - 1) / a.splits);
-    if constexpr (D < 256)
-        if (per_block == 32) return c.page_shift > 4 ? launch_tree_attention<D, true, 2>(c, a, st) : launch_tree_attention<D, false, 2>(c, a, st);
-    return c.page_shift > 4 ? launch_tree_attention<D, true, 1>(c, a, st) : launch_tree_attention<D, false, 1>(c, a, st);
+    auto launch = [&](auto one_page, auto is_packed_) -> sq_status {
+        constexpr bool ONE_PAGE = decltype(one_page)::value, PACKED = decltype(is_packed_)::value;
+        if constexpr (D < 256)
+            if (per_block == 32) return launch_tree_attention<D, ONE_PAGE, 2, PACKED>(c, a, st);
+        return launch_tree_attention<D, ONE_PAGE, 1, PACKED>(c, a, st);
+    };
+    if (is_packed) return c.page_shift > 4 ? launch(std::true_type{}, std::true_type{}) : launch(std::false_type{}, std::true_type{});
+    return c.page_shift > 4 ? launch(std::true_type{}, std::false_type{}) : launch(std::false_type{}, std::false_type{});
 }
 
 }  // namespace

@@ -5,7 +5,7 @@ import pytest
 
 import operators_util as ou
 from parity_util import dev, host
-from test_gpu_operators import rng, rows, run_product, weights
+from test_gpu_operators import Setting, rng, rows, run_product, weights
 
 pytestmark = pytest.mark.gpu
 
@@ -110,3 +110,61 @@ def test_cache_of_more_rows_than_a_row_of_workgroups():
             assert torch.equal(part, x)
     del many, cache
     torch.cuda.empty_cache()
+
+
+# ---- attention: sequences of very different numbers of rows ------------------------------------------
+
+
+RAGGED = [  # past, new, Hq, Hk, D, page, tree
+    ([3] * 30 + [40], [1] * 30 + [100], 8, 2, 64, 16, False), ([0, 5] * 20 + [17, 100], [0, 1] * 20 + [160, 0], 4, 4, 128, 64, False),
+    ([30] * 20 + [2500, 9], [1] * 20 + [60, 2], 8, 1, 128, 32, True), ([200] * 33 + [1], [1] * 33 + [70], 16, 2, 256, 16, False),
+    ([11] * 70, [1] * 69 + [64], 4, 2, 64, 16, True)]
+
+
+@pytest.mark.parametrize("case", range(len(RAGGED)))
+@pytest.mark.parametrize("max_keys", [None, 2 ** 31 - 1])
+def test_attention_of_one_prompt_among_single_rows(case, max_keys):
+    past, new, Hq, Hk, D, page, tree = RAGGED[case]
+    print(f"case attention ragged {case} {max_keys}", flush=True)
+    s = Setting(1300 + case, past, new, Hk, D, page)
+    Q, scale = s.queries(Hq, 2.0), D ** -0.5
+    words = s.trees() if tree else None
+    want, bound = s.expect(Q, Hq // Hk, s.by_mask(words) if tree else s.causal, scale)
+    for workspace in (0, 8 << 20):
+        ou.held(s.run(Q, words, scale, workspace, max_keys=max_keys), want, bound, f"{case} {workspace}")
+    # fewer rows than a sequence has: the others keep what they held
+    most = max(new) - 7
+    over = np.concatenate([np.arange(n) >= most for n in new])
+    got = s.run(Q, words, scale, max_rows=most, max_keys=max_keys)
+    assert (got[over] == 3.0).all()
+    ou.held(got[~over], want[~over], bound[~over], f"{case} max_rows")
+
+
+def test_attention_of_thousands_of_sequences_and_a_prompt():
+    print("case attention 5000 sequences", flush=True)
+    g = rng(42)
+    new = g.integers(0, 2, 5000)
+    new[3210], new[:7], new[-9:] = 90, 0, 0
+    s = Setting(1400, list(g.integers(0, 3, 5000)), list(new), 1, 64, 16)
+    Q = s.queries(2)
+    want, bound = s.expect(Q, 2, s.causal, 0.2)
+    ou.held(s.run(Q, None, 0.2, max_rows=90, max_keys=64), want, bound, "prompt among 5000")
+
+
+def test_attention_of_rows_far_below_their_bound():
+    """2^24 workgroups, were every sequence given row blocks for max_rows, and a launch has fewer."""
+    print("case attention far below max_rows", flush=True)
+    new = [0] * 1024
+    new[0], new[500], new[1023] = 1, 40, 3
+    s = Setting(1500, [2] * 1024, new, 8, 256, 16)
+    import torch
+    import paper_2511_22316_amd as sq
+    Q = s.queries(32)
+    want, bound = s.expect(Q, 4, s.causal, 0.1)
+    T = 8192                                                # rows behind the last sequence
+    q, o = (torch.full((T, 32, 256), 3.0, dtype=torch.float16, device="cuda") for _ in range(2))
+    q[: s.T] = dev(Q)
+    sq.sq_tree_attention(q, s.dstart, s.dcached, None, s.dtable, 16, s.cache, 8, 0.1, o, max_rows=8192)
+    torch.cuda.synchronize()
+    ou.held(host(o[: s.T]), want, bound, "far below")
+    assert (o[s.T:] == 3.0).all()
