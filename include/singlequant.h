@@ -699,6 +699,17 @@ int32_t sq_debug_rotq_plan(const int32_t *giv_i, const int32_t *giv_j, int32_t P
                            int32_t *slot_qslot, int32_t *qslot_q, int32_t *pair_slot_i,
                            int32_t *pair_slot_j, int32_t *pair_level);
 
+/*
+ * sq_debug_tree_attention_plan -- how sq_tree_attention shares a call of these sizes
+ * out.  Host only.  Returns the number of splits of a sequence's keys, or -1 for sizes
+ * that the call refuses; *rows: query rows (times heads of a group) per workgroup; *packed:
+ * whether row blocks are numbered by row_start; *keys: neighbouring keys that a split takes
+ * before it goes on `splits` times as far behind their first one.
+ */
+int32_t sq_debug_tree_attention_plan(int64_t T, int32_t Hq, int32_t Hk, int32_t D, int32_t B,
+                                     int32_t max_rows, int32_t max_keys, int64_t workspace_bytes,
+                                     int32_t *rows, int32_t *packed, int32_t *keys);
+
 #ifdef __cplusplus
 }
 #endif

@@ -589,52 +589,64 @@ sq_status launch_tree_attention(const CacheView &c, const AttentionCall &a, hipS
     return hipGetLastError() == hipSuccess ? SQ_OK : SQ_ERR_LAUNCH;
 }
 
-template <int D>
-sq_status dispatch_tree_attention(const CacheView &c, AttentionCall &a, int64_t max_keys, void *workspace, int64_t workspace_bytes,
-                                  hipStream_t st)
+// How a call is shared out.
+struct AttentionPlan {
+    int rows_per_block;        // 16 R
+    bool packed;
+    int row_blocks, splits, tiles_per_chunk, blocks;
+};
+
+sq_status plan_tree_attention(int64_t T, int Hq, int Hk, int D, int B, int max_rows, int64_t max_keys, int64_t workspace_bytes, AttentionPlan &p)
 {
-    const int64_t rows = (int64_t)a.max_rows * a.group;
+    const int64_t group = Hq / Hk, rows = max_rows * group;
     if (rows > (1 << 30)) return SQ_ERR_SHAPE;
     max_keys = max_keys < 1 ? 1 : max_keys;
     // Row blocks of all sequences: as many as the longest has in each, or packed, where that is less than half (or those are more than
     // one row of a grid).  Us, even / packed, a prompt among sequences of one row (32 heads of 128, 8 of K and V): 2048 rows, 63 others of 2048
     // keys 660 / 91, of 32768 1876 / 612; 64 rows, 32 of 1024 44 / 15; 300 rows, 999 of 300 541 / 130.
-    auto even = [&](int64_t per_block) { return (rows + per_block - 1) / per_block * c.B; };
-    auto packed = [&](int64_t per_block) { return a.T * a.group / per_block + c.B; };
-    auto pack = [&](int64_t per_block) { return 2 * packed(per_block) < even(per_block) || even(per_block) * c.Hk > kGridRow; };
+    auto even = [&](int64_t per_block) { return (rows + per_block - 1) / per_block * B; };
+    auto packed = [&](int64_t per_block) { return T * group / per_block + B; };
+    auto pack = [&](int64_t per_block) { return 2 * packed(per_block) < even(per_block) || even(per_block) * Hk > kGridRow; };
     auto row_blocks = [&](int64_t per_block) { return pack(per_block) ? packed(per_block) : even(per_block); };
     // 32 rows per workgroup from about two waves of work for every SIMD on (us, 16 / 32: 16 sequences, 20 rows, 1024 keys 16.8 /
     // 18.6; one prompt of 300 rows 13.2 / 15.3; 16 sequences, 32 rows, 4096 keys 30.5 / 30.7; one tree of 61 new rows, 16384 keys
     // 44.7 / 39.9; 64 sequences, 28 rows, 8192 keys 122.7 / 103.2).  256 channels of two tiles of rows do not fit in registers.
-    const int64_t per_block = D < 256 && rows > 16 && (double)(row_blocks(16) * c.Hk) * (double)max_keys > 0x1p20 ? 32 : 16;
-    const bool is_packed = pack(per_block);
+    const int64_t per_block = D < 256 && rows > 16 && (double)(row_blocks(16) * Hk) * (double)max_keys > 0x1p20 ? 32 : 16;
     // Splits of the keys: as many as give every CU a workgroup, twice (four times, of many units) that while a split has 2048 keys
     // or more, no more than there are chunks of 128 keys, and none where the keys' tiles take less time than the second launch,
     // about 3 us (us without a split / best / 1024 workgroups, one row of 32 heads per sequence, 8 of K and V, D = 128: one sequence
     // of 512 keys 6.9 / 7.7 / 7.7, of 1024 9.5 / 7.8 / 7.8, of 16384 92 / 11.7 / 13.0; 4 of 4096 26.7 / 11.6 with 8 / 13.5, of 16384
     // 93 / 19.0 with 16 / 20.8; 16 of 1024 10.5 / 11.8 with 2 / 13.3, of 4096 26.9 / 19.5 with 4 / 21.3; 48 of 4096 to 8192 74.2 / 70.6
     // with 2).  And no more than the workspace holds.
-    const int64_t units = row_blocks(per_block) * c.Hk, most = units > 256 && per_block == 16 ? 1024 : 512;
-    const int64_t chunks = (max_keys + kChunkUnit - 1) / kChunkUnit, room = workspace_bytes / (a.T * a.Hq * (D + 2) * 4);
+    const int64_t units = row_blocks(per_block) * Hk, most = units > 256 && per_block == 16 ? 1024 : 512;
+    const int64_t chunks = (max_keys + kChunkUnit - 1) / kChunkUnit, room = workspace_bytes / (T * Hq * (D + 2) * 4);
     int64_t splits = units < 256 ? 256 / units : 1;
     while (2 * splits * units <= most && max_keys >= 2048 * splits) splits *= 2;
     splits = splits < chunks ? splits : chunks;
     splits = splits < kMaxSplits ? splits : kMaxSplits;
     if (max_keys * (splits - 1) < 590 * splits) splits = 1;
     splits = splits < room ? splits : room;
-    a.splits = splits < 1 ? 1 : (int)splits;
-    if (units * a.splits > 0x7FFFFFFF) return SQ_ERR_SHAPE;
-    a.blocks = (int)(units * a.splits);
-    a.row_blocks = (int)(is_packed ? packed(per_block) : even(per_block) / c.B);
-    a.part = static_cast<float *>(workspace);
-    a.tiles_per_chunk = kWaves * (int)((chunks + a.splits - 1) / a.splits);
-    auto launch = [&](auto one_page, auto is_packed_) -> sq_status {
-        constexpr bool ONE_PAGE = decltype(one_page)::value, PACKED = decltype(is_packed_)::value;
+    splits = splits < 1 ? 1 : splits;
+    if (units * splits > 0x7FFFFFFF) return SQ_ERR_SHAPE;
+    p.rows_per_block = (int)per_block;
+    p.packed = pack(per_block);
+    p.row_blocks = (int)(p.packed ? packed(per_block) : even(per_block) / B);
+    p.splits = (int)splits;
+    p.tiles_per_chunk = kWaves * (int)((chunks + splits - 1) / splits);
+    p.blocks = (int)(units * splits);
+    return SQ_OK;
+}
+
+template <int D>
+sq_status dispatch_tree_attention(const CacheView &c, const AttentionCall &a, const AttentionPlan &p, hipStream_t st)
+{
+    auto launch = [&](auto one_page, auto packed) -> sq_status {
+        constexpr bool ONE_PAGE = decltype(one_page)::value, PACKED = decltype(packed)::value;
         if constexpr (D < 256)
-            if (per_block == 32) return launch_tree_attention<D, ONE_PAGE, 2, PACKED>(c, a, st);
+            if (p.rows_per_block == 32) return launch_tree_attention<D, ONE_PAGE, 2, PACKED>(c, a, st);
         return launch_tree_attention<D, ONE_PAGE, 1, PACKED>(c, a, st);
     };
-    if (is_packed) return c.page_shift > 4 ? launch(std::true_type{}, std::true_type{}) : launch(std::false_type{}, std::true_type{});
+    if (p.packed) return c.page_shift > 4 ? launch(std::true_type{}, std::true_type{}) : launch(std::false_type{}, std::true_type{});
     return c.page_shift > 4 ? launch(std::true_type{}, std::false_type{}) : launch(std::false_type{}, std::false_type{});
 }
 
@@ -681,7 +693,29 @@ extern "C" sq_status sq_tree_attention(const void *Q, int64_t ldq, int64_t T, in
     a.max_rows = (int)(max_rows < T ? max_rows : T);
     a.score_scale = (float)((double)scale * 1.4426950408889634 * 1048576.0);
     const hipStream_t st = static_cast<hipStream_t>(stream);
-    if (D == 64) return sq::dispatch_tree_attention<64>(c, a, max_keys, workspace, workspace_bytes, st);
-    if (D == 128) return sq::dispatch_tree_attention<128>(c, a, max_keys, workspace, workspace_bytes, st);
-    return sq::dispatch_tree_attention<256>(c, a, max_keys, workspace, workspace_bytes, st);
+    sq::AttentionPlan p;
+    const sq_status planned = sq::plan_tree_attention(T, Hq, Hk, D, B, a.max_rows, max_keys, workspace_bytes, p);
+    if (planned != SQ_OK) return planned;
+    a.splits = p.splits;
+    a.row_blocks = p.row_blocks;
+    a.blocks = p.blocks;
+    a.tiles_per_chunk = p.tiles_per_chunk;
+    a.part = static_cast<float *>(workspace);
+    if (D == 64) return sq::dispatch_tree_attention<64>(c, a, p, st);
+    if (D == 128) return sq::dispatch_tree_attention<128>(c, a, p, st);
+    return sq::dispatch_tree_attention<256>(c, a, p, st);
+}
+
+extern "C" int32_t sq_debug_tree_attention_plan(int64_t T, int32_t Hq, int32_t Hk, int32_t D, int32_t B, int32_t max_rows, int32_t max_keys,
+                                                int64_t workspace_bytes, int32_t *rows, int32_t *packed, int32_t *keys)
+{
+    if (!rows || !packed || !keys || T <= 0 || T > SQ_MAX_ROWS || Hq <= 0 || Hq > 65536 || max_rows <= 0 || max_keys < 0 || workspace_bytes < 0 || B <= 0 ||
+        sq::check_cache(Hk, D, 16, B, 0, 0) != SQ_OK || Hq % Hk != 0)
+        return -1;
+    sq::AttentionPlan p;
+    if (sq::plan_tree_attention(T, Hq, Hk, D, B, (int)(max_rows < T ? max_rows : T), max_keys, workspace_bytes, p) != SQ_OK) return -1;
+    *rows = p.rows_per_block;
+    *packed = p.packed ? 1 : 0;
+    *keys = p.tiles_per_chunk * sq::kKeysPerTile;
+    return p.splits;
 }

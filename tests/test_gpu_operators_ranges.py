@@ -168,3 +168,69 @@ def test_attention_of_rows_far_below_their_bound():
     torch.cuda.synchronize()
     ou.held(host(o[: s.T]), want, bound, "far below")
     assert (o[s.T:] == 3.0).all()
+
+
+# ---- attention: long sequences, split and shared out in every way ------------------------------------
+
+
+def plan(T, Hq, Hk, D, B, max_rows, max_keys, workspace):
+    """Splits, query rows of a workgroup, whether row blocks are packed, and neighbouring keys of a split."""
+    import ctypes
+    from paper_2511_22316_amd import binding
+    out = [ctypes.c_int32(0) for _ in range(3)]
+    splits = binding._load().sq_debug_tree_attention_plan(T, Hq, Hk, D, B, max_rows, max_keys, workspace, *[ctypes.byref(o) for o in out])
+    return (splits, out[0].value, out[1].value, out[2].value)
+
+
+def held_long(s, got, Q, G, sees_of, scale, what):
+    """As Setting.expect and held, with the term of products below the normal range of fp16 as the kernel's offset has it: where the offset
+    moves, a row's largest product of weight and step is 2^5.9 or more, and it never falls afterwards; a product below the normal range
+    is off by 2^-25 at most, times codes up to 8: n keys by n 2^-22 where the sum of products is 2^5.9 or more, n 2^-27.9 of it.
+    operators_util.attention has n 2^-21, for a largest product of 2^-1."""
+    want, bound = s.expect(Q, G, sees_of, scale)
+    for b in range(s.B):
+        L, rows_ = int(s.past[b] + s.new[b]), slice(s.start[b], s.start[b + 1])
+        if L == 0 or s.new[b] == 0:
+            continue
+        (k, sk), (v, sv) = (s.numbers.values(b, w, L) for w in (0, 1))
+        sees = sees_of(b, L)
+        for h in range(Q.shape[1]):
+            x = np.where(sees, (Q[rows_, h].astype(np.float64) @ k[:, h // G].T) * scale, -np.inf)
+            some = sees.any(1)
+            p = np.zeros(x.shape)
+            p[some] = np.exp(x[some] - x[some].max(1, keepdims=True))
+            p[some] /= p[some].sum(1, keepdims=True)
+            n = sees.sum(1, keepdims=True)
+            bound[rows_, h] -= (1 + ou.HALF) * n * (2.0 ** -21 - 2.0 ** -27.9) * (p @ sv[:, h // G])[:, None]
+    ou.held(got, want, bound, what)
+
+
+LONG = [  # past, new, Hq, Hk, D, page, tree, max_keys: splits, rows, packed of the plan with a workspace
+    ([9000], [61], 8, 2, 64, 16, True, 40000, (32, 32, 0)),                          # 32 rows, eight splits of 1280 keys with something in them
+    ([9000], [61], 8, 2, 128, 64, True, 40000, (32, 32, 0)),
+    ([300, 12000, 0, 50, 900, 31, 2, 40], [61, 60, 64, 1, 7, 33, 50, 12], 8, 2, 64, 32, True, 4200, (4, 32, 0)),     # the next chunk, three times
+    ([7000, 20], [64, 64], 16, 4, 128, 16, True, 8300, (8, 32, 0)),
+    ([3000, 900, 0, 2500], [1, 1, 1, 1], 8, 2, 64, 16, False, 1024, (8, 16, 0)),     # 16 rows, the next chunk
+    ([3000, 900, 0, 2500], [1, 1, 0, 1], 8, 2, 256, 64, False, 1024, (8, 16, 0)),
+    ([2100, 5], [9, 3], 8, 1, 128, 32, True, 1024, (8, 16, 0)),
+    ([40] * 9 + [6000, 0], [1] * 9 + [50, 1], 4, 1, 64, 16, True, 45000, (28, 32, 1)),      # packed and split
+    ([16383], [1], 4, 1, 128, 64, False, None, (64, 16, 0)), ([20000], [1], 2, 2, 64, 16, False, 20001, (64, 16, 0)),
+    ([100], [2048], 4, 1, 64, 64, False, None, (2, 32, 0)), ([0, 700], [2100, 513], 2, 1, 128, 16, False, None, (1, 32, 0)),
+    ([0], [4100], 2, 1, 128, 32, False, None, (1, 32, 0)), ([50], [1100], 2, 1, 256, 16, False, None, (1, 16, 0))]
+
+
+@pytest.mark.parametrize("case", range(len(LONG)))
+def test_attention_of_long_sequences(case):
+    past, new, Hq, Hk, D, page, tree, max_keys, how = LONG[case]
+    print(f"case attention long {LONG[case]}", flush=True)
+    s = Setting(1600 + case, past, new, Hk, D, page)
+    hint, workspace = s.per * page if max_keys is None else max_keys, 64 << 20
+    assert plan(s.T, Hq, Hk, D, s.B, max(new), hint, workspace)[:3] == how
+    if max_keys is not None and how[0] > 1:
+        splits, _, _, keys = plan(s.T, Hq, Hk, D, s.B, max(new), hint, workspace)
+        assert max(past) > 2 * keys                         # several splits have keys of their own
+    Q, scale = s.queries(Hq, 2.0), D ** -0.5
+    words = s.trees() if tree else None
+    sees = s.by_mask(words) if tree else s.causal
+    for ws in (workspace, 0):
+        held_long(s, s.run(Q, words, scale, ws, max_keys=max_keys), Q, Hq // Hk, sees, scale, f"{case} {ws}")

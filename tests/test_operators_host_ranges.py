@@ -61,3 +61,25 @@ def test_grouped_product_refuses_more_channels_than_it_numbers(lib):
             for group in (32, 256):
                 assert lib.sq_w4a16_gemm_grouped(FAKE, T, 256, 256, FAKE, FAKE, group, N, FAKE, N, None) == SHAPE, (T, N, group)
     assert lib.sq_w4a16_gemm_grouped(FAKE, 1 << 24, 256, 256, FAKE, FAKE, 64, 1 << 28, FAKE, 1 << 28, None) == SHAPE     # 2^37 tiles
+
+
+def test_attention_plan(lib):
+    """What the rules of a call's sizes say, without a GPU: refusals, and workgroups that a launch can count."""
+    import ctypes
+    out = [ctypes.c_int32(0) for _ in range(3)]
+    def plan(T=64, Hq=32, Hk=8, D=128, B=64, max_rows=1, max_keys=4096, workspace=64 << 20):
+        splits = lib.sq_debug_tree_attention_plan(T, Hq, Hk, D, B, max_rows, max_keys, workspace, *[ctypes.byref(o) for o in out])
+        return (splits, *[o.value for o in out])
+    for bad in (dict(T=0), dict(T=-1), dict(Hq=31), dict(Hk=0), dict(D=96), dict(B=0), dict(max_rows=0), dict(max_keys=-1), dict(workspace=-1)):
+        assert plan(**bad)[0] == -1, bad
+    assert plan()[:3] == (2, 16, 0) and plan(max_keys=2000)[:3] == (1, 16, 0)        # 512 workgroups for the sequences, twice for long ones
+    assert plan(T=1, B=1, max_keys=16384)[:3] == (32, 16, 0) and plan(T=1, B=1, max_keys=16384, workspace=0)[0] == 1
+    assert plan(T=61, B=1, max_rows=61, max_keys=16384)[:3] == (8, 32, 0)
+    assert plan(T=16 * 61, B=16, max_rows=61)[:3] == (1, 32, 0)
+    assert plan(T=2111, B=64, max_rows=2048, max_keys=32768)[:3] == (1, 32, 1)
+    assert plan(T=8192, B=1024, max_rows=8192, D=256)[:3] == (1, 16, 1)
+    # keys of a split times splits hold max_keys, whatever it is
+    for keys in (0, 1, 127, 129, 1000, 4097, 70000, 2 ** 31 - 1):
+        for T in (1, 3, 40):
+            splits, _, _, each = plan(T=T, B=T, max_keys=keys)
+            assert 1 <= splits <= 64 and splits * each >= keys and each % 128 == 0
