@@ -700,6 +700,15 @@ int32_t sq_debug_rotq_plan(const int32_t *giv_i, const int32_t *giv_j, int32_t P
                            int32_t *pair_slot_j, int32_t *pair_level);
 
 /*
+ * sq_debug_grouped_plan -- which kernel sq_w4a16_gemm_grouped takes for these sizes.  Host
+ * only.  1 .. 4: the kernel for few tokens with 16, 32 or 64 channels per workgroup, or 64 and
+ * two blocks of 16 tokens; 5: token rows in LDS; 6, 7: token rows in parts, eight or two
+ * blocks of 16 channels side by side; 8 .. 11: tiles of 64 x 128, 128 x 128, 128 x 256 or 256 x 256
+ * tokens x channels; 0: no launch.
+ */
+int32_t sq_debug_grouped_plan(int64_t T, int32_t K, int32_t group, int32_t N);
+
+/*
  * sq_debug_tree_attention_plan -- how sq_tree_attention shares a call of these sizes
  * out.  Host only.  Returns the number of splits of a sequence's keys, or -1 for sizes
  * that the call refuses; *rows: query rows (times heads of a group) per workgroup; *packed:

@@ -162,6 +162,8 @@ def _load():
             C.c_void_p, C.c_int64, C.c_int64, C.c_int32, C.c_int32, C.c_int32,
             C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p, C.c_int32, C.c_int32, C.c_void_p, C.c_int32, C.c_int32,
             C.c_void_p, C.c_int32, C.c_float, C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_void_p]
+        lib.sq_debug_grouped_plan.restype = C.c_int32
+        lib.sq_debug_grouped_plan.argtypes = [C.c_int64, C.c_int32, C.c_int32, C.c_int32]
         lib.sq_debug_tree_attention_plan.restype = C.c_int32
         lib.sq_debug_tree_attention_plan.argtypes = [
             C.c_int64, C.c_int32, C.c_int32, C.c_int32, C.c_int32, C.c_int32, C.c_int32, C.c_int64, C.c_void_p, C.c_void_p, C.c_void_p]

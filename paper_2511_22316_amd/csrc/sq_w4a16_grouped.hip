@@ -587,31 +587,34 @@ sq_status launch_grouped_parts(const GroupedArgs &a)
     return hipGetLastError() == hipSuccess ? SQ_OK : SQ_ERR_LAUNCH;
 }
 
-template <int GROUP>
-sq_status launch_grouped_few(const GroupedArgs &a)
+// The kernels and their shapes, numbered as sq_debug_grouped_plan has them.
+enum GroupedKernel {
+    kChannels16 = 1, kChannels32, kChannels64, kChannels64Tokens32,        // per workgroup of the kernel for few tokens
+    kRowsInLds,
+    kParts8, kParts2,                                                      // blocks of channels side by side
+    kTiles64x128, kTiles128x128, kTiles128x256, kTiles256x256
+};
+
+GroupedKernel choose_grouped_few(int64_t T, int K, int64_t N)
 {
-    const int64_t tiles = (a.T + 15) / 16, blocks = (a.N + 15) / 16;
-    const bool slices = a.K % 128 == 0, large = (int64_t)a.K * a.N > ((int64_t)32 << 20) && blocks > 256;
+    const int64_t tiles = (T + 15) / 16, blocks = (N + 15) / 16;
+    const bool slices = K % 128 == 0, large = K * N > ((int64_t)32 << 20) && blocks > 256;
     // Token rows in LDS where they fit and there is enough to share out evenly (us, that / the kernel for few tokens at its best,
     // T = 1, groups of 128: K = 4096, N = 8192 9.0 / 7.7, N = 9216 10.3 / 12.0; K = 8192, N = 8192 12.7 / 13.7, N = 28672 28.9 / 38.0),
     // at more than one block of channels per workgroup (K = 11008, N = 4096 10.9 / 10.1).
-    if (tiles == 1 && slices && large && (int64_t)a.T * row_bytes(a.K, 512) <= kMaxDynamicLds) return launch_grouped_rows<GROUP, 8, 4>(a);
+    if (tiles == 1 && slices && large && T * row_bytes(K, 512) <= kMaxDynamicLds) return kRowsInLds;
     // In parts where they do not fit, or are more than 16 over a K worth the two barriers of a part (us, parts / the kernel for few
     // tokens, groups of 128: T = 16, K = 8192, N = 28672 30.7 / 47.8, K = 5120, N = 13824 15.0 / 17.5, K = 8192, N = 8192 16.2 / 18.2, but
     // T = 8, K = 28672, N = 8192 42.1 / 39.3; T = 32, K = 1024, N = 28672 9.1 / 12.4, N = 16384 7.4 / 7.2; K = 2048, N = 16384 9.9 / 11.6;
     // K = 4096, N = 8192 11.9 / 13.9).
-    if (slices && blocks > 256 && (tiles == 2 ? a.K >= (blocks > 1024 ? 1024 : 2048) : tiles == 1 && large && (a.T > 8 || blocks > 512))) {
-        if (blocks > 512) return tiles == 2 ? launch_grouped_parts<GROUP, 2, 8, 2>(a) : launch_grouped_parts<GROUP, 1, 8, 2>(a);
-        return tiles == 2 ? launch_grouped_parts<GROUP, 2, 2, 8>(a) : launch_grouped_parts<GROUP, 1, 2, 8>(a);
-    }
+    if (slices && blocks > 256 && (tiles == 2 ? K >= (blocks > 1024 ? 1024 : 2048) : tiles == 1 && large && (T > 8 || blocks > 512)))
+        return blocks > 512 ? kParts8 : kParts2;
     // The fewest channels per workgroup that need one round of workgroups on the 256 CUs (us with 16 / 32 / 64 channels, T = 1,
     // K = 4096, groups of 128: N = 4096 5.8 / 7.4 / 11.8, N = 6144 9.0 / 7.5 / 12.0, N = 9216 12.2 / 12.7 / 12.0), and both blocks of
-    // 16 tokens in a workgroup before there are two rounds (T = 32, N = 11008 26.0 / 19.8).  Groups of 32 and 64 have more
-    // registers of steps: a slice at a time then fits.
-    if (blocks * tiles <= 256) return launch_grouped_skinny<GROUP, 1, 8, 1, 2>(a);
-    if (blocks * tiles <= 512) return launch_grouped_skinny<GROUP, 2, 8, 1, 2>(a);
-    if (tiles == 1 || blocks * tiles <= 1024) return launch_grouped_skinny<GROUP, 4, 8, 1, GROUP <= 64 ? 1 : 2>(a);
-    return launch_grouped_skinny<GROUP, 4, 8, 2, 1>(a);
+    // 16 tokens in a workgroup before there are two rounds (T = 32, N = 11008 26.0 / 19.8).
+    if (blocks * tiles <= 256) return kChannels16;
+    if (blocks * tiles <= 512) return kChannels32;
+    return tiles == 1 || blocks * tiles <= 1024 ? kChannels64 : kChannels64Tokens32;
 }
 
 // Many tokens: the tile kernel of sq_w4a16_gemm with the steps on the widened codes.  Us per shape, groups of 128:
@@ -622,19 +625,53 @@ sq_status launch_grouped_few(const GroupedArgs &a)
 //                             that is less: T = 4096, K = 11008, N = 4096 351 (389), T = 1500, K = 4096, N = 14336 218 (184)
 // T = 2048, K = N = 4096 takes 74.5 us with groups of 32 or 64 (sq_w4a16_gemm with its step per channel 65), T = 333, K = 5120,
 // N = 13824 69 (60): what the steps cost is the packed multiplication per two codes and power.
-sq_status launch_grouped_many(const GroupedArgs &a)
+GroupedKernel choose_grouped_many(int64_t T, int K, int64_t N)
 {
-    const int shift = __builtin_ctz((unsigned)a.group);
-    auto tiles = [&](int bm, int bn) { return ((int64_t)a.T + bm - 1) / bm * (((int64_t)a.N + bn - 1) / bn); };
+    auto tiles = [&](int bm, int bn) { return (T + bm - 1) / bm * ((N + bn - 1) / bn); };
     auto rounds = [&](int bm, int bn) { return (tiles(bm, bn) + 255) / 256; };
-    const bool two_k_groups = a.K % 128 == 0;
-    if (two_k_groups && (a.T <= 64 || tiles(64, 128) <= 256))
-        return launch_w4a16_ring<1, 4, 2, 1, 1, 64, 0, 2, true>(a.X, a.ldx, a.T, a.K, a.Qw, a.steps, a.N, a.Y, a.ldy, a.st, shift);
-    if (two_k_groups && tiles(128, 128) <= 256)
-        return launch_w4a16_ring<1, 4, 4, 1, 1, 64, 0, 2, true>(a.X, a.ldx, a.T, a.K, a.Qw, a.steps, a.N, a.Y, a.ldy, a.st, shift);
-    if (37 * rounds(256, 256) < 20 * rounds(128, 256))
-        return launch_w4a16_ring<2, 4, 4, 2, 1, 64, 0, 1, true>(a.X, a.ldx, a.T, a.K, a.Qw, a.steps, a.N, a.Y, a.ldy, a.st, shift);
-    return launch_w4a16_ring<1, 4, 4, 2, 1, 64, 4, 1, true>(a.X, a.ldx, a.T, a.K, a.Qw, a.steps, a.N, a.Y, a.ldy, a.st, shift);
+    const bool two_k_groups = K % 128 == 0;
+    if (two_k_groups && (T <= 64 || tiles(64, 128) <= 256)) return kTiles64x128;
+    if (two_k_groups && tiles(128, 128) <= 256) return kTiles128x128;
+    return 37 * rounds(256, 256) < 20 * rounds(128, 256) ? kTiles256x256 : kTiles128x256;
+}
+
+GroupedKernel choose_grouped(int64_t T, int K, int64_t N)
+{
+    // Tiles of many tokens, but where the kernel for few needs one round of workgroups for them all: a workgroup there shares K
+    // among eight waves, a tile is one walk over it (us, few / tiles, groups of 128: T = 64, K = 4096, N = 1024 7.8 / 23.8, T = 128,
+    // N = 4096 19.4 / 24.4, K = 11008 38.8 / 62.9; two rounds: T = 48, N = 11008 33.3 / 26.1, T = 128, N = 8192 35.7 / 25.4).
+    if (T > 32 && (T + 31) / 32 * ((N + 63) / 64) > 256) return choose_grouped_many(T, K, N);
+    return choose_grouped_few(T, K, N);
+}
+
+template <int GROUP>
+sq_status launch_grouped_few(const GroupedArgs &a, GroupedKernel kernel)
+{
+    const bool two = a.T > 16;
+    switch (kernel) {
+        case kRowsInLds: return launch_grouped_rows<GROUP, 8, 4>(a);
+        case kParts8: return two ? launch_grouped_parts<GROUP, 2, 8, 2>(a) : launch_grouped_parts<GROUP, 1, 8, 2>(a);
+        case kParts2: return two ? launch_grouped_parts<GROUP, 2, 2, 8>(a) : launch_grouped_parts<GROUP, 1, 2, 8>(a);
+        case kChannels16: return launch_grouped_skinny<GROUP, 1, 8, 1, 2>(a);
+        case kChannels32: return launch_grouped_skinny<GROUP, 2, 8, 1, 2>(a);
+        // groups of 32 and 64 have more registers of steps: a slice at a time then fits
+        case kChannels64: return launch_grouped_skinny<GROUP, 4, 8, 1, GROUP <= 64 ? 1 : 2>(a);
+        default: return launch_grouped_skinny<GROUP, 4, 8, 2, 1>(a);
+    }
+}
+
+template <int WM, int FM, int FN, int LW, int KG>
+sq_status launch_grouped_tiles(const GroupedArgs &a)
+{
+    return launch_w4a16_ring<WM, 4, FM, FN, 1, 64, LW, KG, true>(a.X, a.ldx, a.T, a.K, a.Qw, a.steps, a.N, a.Y, a.ldy, a.st, __builtin_ctz((unsigned)a.group));
+}
+
+sq_status check_grouped(int64_t T, int32_t K, int32_t group, int32_t N)
+{
+    if (group != 32 && group != 64 && group != 128 && group != 256) return SQ_ERR_SHAPE;
+    if (T < 0 || N < 0 || K <= 0 || (K % 64) != 0 || (K % group) != 0 || K > 131072) return SQ_ERR_SHAPE;
+    if (T > (1 << 24) || N > (1 << 28)) return SQ_ERR_SHAPE;         // 2^28 channels: their numbers, padded, and the grids stay in 32 bits
+    return SQ_OK;
 }
 
 }  // namespace
@@ -644,21 +681,28 @@ sq_status launch_grouped_many(const GroupedArgs &a)
 extern "C" sq_status sq_w4a16_gemm_grouped(const void *X, int64_t T, int32_t K, int64_t ldx, const uint8_t *Qw,
                                            const void *steps, int32_t group, int32_t N, void *Y, int64_t ldy, void *stream)
 {
-    if (group != 32 && group != 64 && group != 128 && group != 256) return SQ_ERR_SHAPE;
-    if (T < 0 || N < 0 || K <= 0 || (K % 64) != 0 || (K % group) != 0 || K > 131072) return SQ_ERR_SHAPE;
-    if (T > (1 << 24) || N > (1 << 28) || ldx < K || ldy < N) return SQ_ERR_SHAPE;      // 2^28 channels: their numbers, padded, and the grids stay in 32 bits
+    const sq_status shape = sq::check_grouped(T, K, group, N);
+    if (shape != SQ_OK) return shape;
+    if (ldx < K || ldy < N) return SQ_ERR_SHAPE;
     if (T == 0 || N == 0) return SQ_OK;
     if (!X || !Qw || !steps || !Y) return SQ_ERR_NULL;
     if (((uintptr_t)X & 15) || (ldx % 8) != 0 || ((uintptr_t)Qw & 15) || ((uintptr_t)Y & 1) || ((uintptr_t)steps & (group == 32 ? 3 : 1)))
         return SQ_ERR_ALIGN;
     const sq::GroupedArgs a = {static_cast<const __half *>(X), ldx, (int)T, K, Qw, static_cast<const __half *>(steps), group, N,
                                static_cast<__half *>(Y), ldy, static_cast<hipStream_t>(stream)};
-    // Tiles of many tokens, but where the kernel for few needs one round of workgroups for them all: a workgroup there shares K
-    // among eight waves, a tile is one walk over it (us, few / tiles, groups of 128: T = 64, K = 4096, N = 1024 7.8 / 23.8, T = 128,
-    // N = 4096 19.4 / 24.4, K = 11008 38.8 / 62.9; two rounds: T = 48, N = 11008 33.3 / 26.1, T = 128, N = 8192 35.7 / 25.4).
-    if (T > 32 && (T + 31) / 32 * (((int64_t)N + 63) / 64) > 256) return sq::launch_grouped_many(a);
-    if (group == 32) return sq::launch_grouped_few<32>(a);
-    if (group == 64) return sq::launch_grouped_few<64>(a);
-    if (group == 128) return sq::launch_grouped_few<128>(a);
-    return sq::launch_grouped_few<256>(a);
+    const sq::GroupedKernel kernel = sq::choose_grouped(T, K, N);
+    if (kernel == sq::kTiles64x128) return sq::launch_grouped_tiles<1, 2, 1, 0, 2>(a);
+    if (kernel == sq::kTiles128x128) return sq::launch_grouped_tiles<1, 4, 1, 0, 2>(a);
+    if (kernel == sq::kTiles128x256) return sq::launch_grouped_tiles<1, 4, 2, 4, 1>(a);
+    if (kernel == sq::kTiles256x256) return sq::launch_grouped_tiles<2, 4, 2, 0, 1>(a);
+    if (group == 32) return sq::launch_grouped_few<32>(a, kernel);
+    if (group == 64) return sq::launch_grouped_few<64>(a, kernel);
+    if (group == 128) return sq::launch_grouped_few<128>(a, kernel);
+    return sq::launch_grouped_few<256>(a, kernel);
+}
+
+extern "C" int32_t sq_debug_grouped_plan(int64_t T, int32_t K, int32_t group, int32_t N)
+{
+    if (T == 0 || N == 0 || sq::check_grouped(T, K, group, N) != SQ_OK) return 0;
+    return (int32_t)sq::choose_grouped(T, K, N);
 }

@@ -57,6 +57,26 @@ def test_product_of_steps_that_are_not_finite():
         ou.held(got[:, ~there], want[:, ~there], bound[:, ~there], f"{T} {N}")
 
 
+KERNELS = {  # what sq_debug_grouped_plan says: shapes (T, K, N), K an odd multiple of 256 (a half of it begins inside a group)
+    1: [(5, 768, 1000), (33, 256, 500)], 2: [(1, 1280, 6000)], 3: [(3, 768, 9000)], 4: [(30, 768, 9000), (250, 768, 2040)],
+    5: [(5, 4864, 7200)], 6: [(20, 1280, 16600), (15, 5376, 9000)], 7: [(20, 2304, 5000), (12, 8448, 5000)],
+    8: [(64, 768, 8300)], 9: [(300, 768, 8200)], 10: [(600, 768, 9000)], 11: [(1000, 768, 9000)]}
+
+
+@pytest.mark.parametrize("group", [32, 64, 128, 256])
+@pytest.mark.parametrize("kernel", sorted(KERNELS))
+def test_product_on_every_kernel(kernel, group):
+    """Every kernel with every group, and the shape that is meant to take it takes it."""
+    from paper_2511_22316_amd import binding
+    for T, K, N in KERNELS[kernel]:
+        print(f"case product kernel {kernel} {T} {K} {N} {group}", flush=True)
+        assert binding._load().sq_debug_grouped_plan(T, K, group, N) == kernel
+        g = rng(32, T, K, N, group)
+        X, (codes, steps) = rows(g, T, K), weights(g, N, K, group)
+        want, bound = ou.product(X, codes, steps, group, T > 32)
+        ou.held(run_product(X, codes, steps, 8, 3), want, bound, f"{kernel} {T} {K} {N} {group}")
+
+
 # ---- more threads than a launch counts along x -------------------------------------------------------
 
 

@@ -83,3 +83,14 @@ def test_attention_plan(lib):
         for T in (1, 3, 40):
             splits, _, _, each = plan(T=T, B=T, max_keys=keys)
             assert 1 <= splits <= 64 and splits * each >= keys and each % 128 == 0
+
+
+def test_grouped_plan(lib):
+    """Which kernel a product takes: the shapes that the GPU tests mean for each of them."""
+    from test_gpu_operators_ranges import KERNELS
+    for kernel, shapes in KERNELS.items():
+        for T, K, N in shapes:
+            for group in (32, 64, 128, 256):
+                assert lib.sq_debug_grouped_plan(T, K, group, N) == kernel, (T, K, N, group)
+    for bad in ((0, 256, 32, 8), (4, 256, 32, 0), (-1, 256, 32, 8), (4, 96, 32, 8), (4, 256, 48, 8), (4, 320, 128, 8), (4, 256, 32, (1 << 28) + 1)):
+        assert lib.sq_debug_grouped_plan(*bad) == 0, bad
