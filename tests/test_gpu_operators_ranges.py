@@ -77,6 +77,19 @@ def test_product_on_every_kernel(kernel, group):
         ou.held(run_product(X, codes, steps, 8, 3), want, bound, f"{kernel} {T} {K} {N} {group}")
 
 
+
+@pytest.mark.parametrize("T,K,N,group", [(4, 512, 100, 64), (40, 512, 300, 32), (64, 512, 8300, 128), (100, 320, 8300, 32)])
+def test_product_of_small_steps(T, K, N, group):
+    """Steps below the normal range of fp16, whose codes times the step are below it too."""
+    print(f"case product small steps {T} {K} {N} {group}", flush=True)
+    g = rng(33, T, K, N, group)
+    X = rows(g, T, K)
+    codes = g.integers(-8, 8, (N, K))
+    steps = (np.floor(2.0 ** g.uniform(0, 11, (N, K // group))) * 2.0 ** -24).astype(np.float16)
+    want, bound = ou.product(X, codes, steps, group, T > 32)
+    assert (bound < 0.2 * np.abs(want)).mean() > 0.7        # a number flushed to zero would be seen
+    ou.held(run_product(X, codes, steps), want, bound, f"{T} {K} {N} {group}")
+
 # ---- more threads than a launch counts along x -------------------------------------------------------
 
 
