@@ -90,6 +90,42 @@ def test_product_of_small_steps(T, K, N, group):
     assert (bound < 0.2 * np.abs(want)).mean() > 0.7        # a number flushed to zero would be seen
     ou.held(run_product(X, codes, steps), want, bound, f"{T} {K} {N} {group}")
 
+
+@pytest.mark.parametrize("T,group", [(1, 32), (20, 64), (300, 128), (40, 256)])
+def test_layer_by_rotation_group_quantizer_and_product(T, group):
+    """X W = (X R)(R^T W): rows of W^T and of X through the layer's own rotation, W to codes with steps per group, and the product of
+    both.  R1 and R2 are Hadamard matrices / 4 and the rotated weights whole multiples -7 .. 7 of a power of two per group (7 among
+    them), so every stage is exact: the weights before are multiples of 2^-4 of it below 2^11, the rotated X multiples of 2^-4 below 2^7,
+    and the result is the fp16 next to X W."""
+    import torch
+    import paper_2511_22316_amd as sq
+    print(f"case layer {T} {group}", flush=True)
+    g = rng(34, T, group)
+    K, N, n = 256, 300, 16
+    H = np.array([[1.0]])
+    while len(H) < n:
+        H = np.block([[H, H], [H, -H]])
+    R = np.kron(H / 4, H / 4)                               # x' = R1^T X_mat R2, row-major
+    codes = g.integers(-7, 8, (N, K // group, group))
+    codes[:, :, 5] = 7
+    steps = 2.0 ** -g.integers(3, 5, (N, K // group)).astype(np.float64)
+    rotated = (codes * steps[..., None]).reshape(N, K)
+    Wt, X = rotated @ R.T, g.integers(-7, 8, (T, K)).astype(np.float64)
+    assert np.array_equal(Wt, Wt.astype(np.float16)) and np.array_equal(X @ R, (X @ R).astype(np.float16))
+    dR = dev((H / 4).astype(np.float16))
+    out = []
+    for x in (Wt, X):
+        y = torch.empty(*x.shape, dtype=torch.float16, device="cuda")
+        sq.sq_rotate_fp16(dev(x.astype(np.float16)), np.zeros(0, np.int32), np.zeros(0, np.int32), np.zeros(0, np.float32), dR, dR, y)
+        out.append(y)
+    Qw = torch.empty(N, K // 2, dtype=torch.uint8, device="cuda")
+    sw = torch.empty(N, K // group, dtype=torch.float16, device="cuda")
+    Y = torch.empty(T, N, dtype=torch.float16, device="cuda")
+    sq.sq_quantize_grouped(out[0], group, Qw, sw)
+    sq.sq_w4a16_gemm_grouped(out[1], Qw, sw, Y)
+    assert np.array_equal(host(sw), steps) and np.array_equal(host(Qw), ou.pack(codes.reshape(N, K)))
+    assert np.array_equal(host(Y), (X @ Wt.T).astype(np.float16))
+
 # ---- more threads than a launch counts along x -------------------------------------------------------
 
 
