@@ -47,7 +47,9 @@ def _load():
         import torch
         _torch = torch
         _f16, _u8, _i32, _i64 = torch.float16, torch.uint8, torch.int32, torch.int64
-        _raw_stream, _raw_device = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice
+        # short ways to the current stream and device, where this torch has them
+        _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda device: torch.cuda.current_stream(device).cuda_stream)
+        _raw_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
         lib = C.CDLL(_LIB_PATH)
         lib.sq_rotate_quantize.restype = C.c_int
         lib.sq_rotate_quantize.argtypes = [

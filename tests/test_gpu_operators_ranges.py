@@ -77,7 +77,6 @@ def test_product_on_every_kernel(kernel, group):
         ou.held(run_product(X, codes, steps, 8, 3), want, bound, f"{kernel} {T} {K} {N} {group}")
 
 
-
 @pytest.mark.parametrize("T,K,N,group", [(4, 512, 100, 64), (40, 512, 300, 32), (64, 512, 8300, 128), (100, 320, 8300, 32)])
 def test_product_of_small_steps(T, K, N, group):
     """Steps below the normal range of fp16, whose codes times the step are below it too."""
@@ -125,6 +124,7 @@ def test_layer_by_rotation_group_quantizer_and_product(T, group):
     sq.sq_w4a16_gemm_grouped(out[1], Qw, sw, Y)
     assert np.array_equal(host(sw), steps) and np.array_equal(host(Qw), ou.pack(codes.reshape(N, K)))
     assert np.array_equal(host(Y), (X @ Wt.T).astype(np.float16))
+
 
 # ---- more threads than a launch counts along x -------------------------------------------------------
 

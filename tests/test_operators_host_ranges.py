@@ -94,3 +94,18 @@ def test_grouped_plan(lib):
                 assert lib.sq_debug_grouped_plan(T, K, group, N) == kernel, (T, K, N, group)
     for bad in ((0, 256, 32, 8), (4, 256, 32, 0), (-1, 256, 32, 8), (4, 96, 32, 8), (4, 256, 48, 8), (4, 320, 128, 8), (4, 256, 32, (1 << 28) + 1)):
         assert lib.sq_debug_grouped_plan(*bad) == 0, bad
+
+
+def test_library_loads_without_torch_names_of_its_own_gpu_build(lib, monkeypatch):
+    """Host-only calls need no more of torch than its tensors; a torch without GPU has no device and stream calls of its own."""
+    import torch
+    for name in ("_cuda_getCurrentRawStream", "_cuda_getDevice"):
+        monkeypatch.delattr(torch._C, name, raising=False)
+    for name in ("_lib", "_raw_stream", "_raw_device"):
+        monkeypatch.setattr(binding, name, None)
+    assert sq.sq_kron_factor(4096) == (64, 64)
+    assert sq.sq_status_string(0) == "ok" and sq.sq_cache_page_bytes(8, 128, 64) == 8 * 64 * 132
+    x = torch.zeros(2, 64, dtype=torch.float16)
+    with pytest.raises(ValueError, match="device"):
+        sq.sq_quantize_grouped(x, 32, torch.zeros(2, 32, dtype=torch.uint8), torch.zeros(2, 2, dtype=torch.float16))
+    assert binding._raw_device is torch.cuda.current_device and callable(binding._raw_stream)
