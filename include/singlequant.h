@@ -529,7 +529,8 @@ sq_status sq_rotary_fp16(const void *X, int64_t T, int32_t H, int32_t D, int64_t
  *   Hk         heads of K and V, 1 .. SQ_CACHE_MAX_HEADS; D 64, 128 or 256
  *   page       a power of two, 16 .. 1024; pages >= 0
  *   B          0 .. SQ_CACHE_MAX_SEQUENCES
- *   row_start  device, int32 [B + 1], not decreasing
+ *   row_start  device, int32 [B + 1], not decreasing; a sequence that begins below 0 is
+ *              left out
  *   cached     device, int32 [B]; below zero: a sequence without keys, whose rows are
  *              left out
  *   table      device, int32 [B, per_sequence]; page * per_sequence < 2^31

@@ -11,7 +11,7 @@ namespace {
 __device__ __forceinline__ uint8_t *place_of_row(const CacheView &c, int64_t row, int &slot)
 {
     const RowOwner r = owner_of_row(c, row);
-    if (r.b < 0 || r.cached < 0) return nullptr;
+    if (r.b < 0 || r.first < 0 || r.cached < 0) return nullptr;
     const int64_t at = (int64_t)r.cached + (row - r.first);
     if (at >= ((int64_t)c.per_sequence << c.page_shift)) return nullptr;
     slot = (int)at & ((1 << c.page_shift) - 1);

@@ -303,3 +303,29 @@ def test_attention_of_long_sequences(case):
     sees = s.by_mask(words) if tree else s.causal
     for ws in (workspace, 0):
         held_long(s, s.run(Q, words, scale, ws, max_keys=max_keys), Q, Hq // Hk, sees, scale, f"{case} {ws}")
+
+
+def test_a_sequence_that_begins_below_zero_is_left_out():
+    """By all three calls alike, also where row blocks are numbered by row_start."""
+    import torch
+    import paper_2511_22316_amd as sq
+    print("case row_start below zero", flush=True)
+    Hk, D, page = 1, 64, 16
+    for B in (2, 40):
+        start = np.minimum(np.array([-2, 1] + [3 + b for b in range(B - 1)]), 41).astype(np.int32)
+        T = int(start[-1]) + 60
+        x = rows(rng(43, B), T, Hk * D).reshape(T, Hk, D)
+        args = dev(start), dev(np.zeros(B, np.int32)), dev(np.arange(B, dtype=np.int32)[:, None]), page
+        cache = torch.full((B, sq.sq_cache_page_bytes(Hk, D, page)), 0x77, dtype=torch.uint8, device="cuda")
+        sq.sq_cache_append(dev(x), dev(x), *args, cache)
+        assert (cache[0] == 0x77).all()
+        k, v, o = (torch.full((T, Hk, D), 3.0, dtype=torch.float16, device="cuda") for _ in range(3))
+        sq.sq_cache_read(cache, *args, k, v)
+        sq.sq_tree_attention(dev(x), *args[:2], None, *args[2:], cache, Hk, 0.1, o, max_rows=T)
+        codes, steps = ou.quantize(x)
+        want = (codes * steps.astype(np.float64)[..., None]).astype(np.float16)
+        own = np.arange(T) >= 1
+        own[start[-1]:] = False
+        for got in (k, v):
+            assert np.array_equal(host(got)[own], want[own]) and (host(got)[~own] == 3.0).all()
+        assert (host(o)[~own] == 3.0).all() and not (host(o)[own] == 3.0).all()
