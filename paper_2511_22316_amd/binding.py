@@ -564,8 +564,8 @@ def sq_rotary_table(rot, base=10000.0, scaling=SQ_ROTARY_PLAIN, factor=1.0, trai
     """The frequencies of rot / 2 pairs as fractions of a turn in units of 2^-64: int64 [rot / 2] on the host (the bits of
     the unsigned numbers), to be copied to the device for sq_rotary_fp16."""
     lib = _load()
-    rot = int(rot)
-    turns = np.zeros(max(rot, 0) // 2, np.int64)
+    rot = min(int(rot), 0x7FFFFFFE)                        # refused there; beyond 32 bits ctypes would take the lower ones
+    turns = np.zeros(max(rot, 0) // 2 if rot < 65536 else 0, np.int64)
     _check(lib.sq_rotary_table(rot, float(base), int(scaling), float(factor), float(trained), float(low), float(high),
                                turns.ctypes.data))
     return _torch.from_numpy(turns)
@@ -594,8 +594,16 @@ def sq_rotary_fp16(X, positions, turns, half, Y, magnitude=1.0, stream=None) -> 
         _check(code)
 
 
+def _int32(**numbers):
+    for name, v in numbers.items():
+        if not -0x80000000 <= v <= 0x7FFFFFFF:
+            raise ValueError(f"{name} must fit in 32 bits")
+
+
 @functools.lru_cache(maxsize=256)
 def sq_cache_page_bytes(Hk: int, D: int, page: int) -> int:
+    if max(Hk, D, page) > 0x7FFFFFFF:
+        return 0
     return int(_load().sq_cache_page_bytes(int(Hk), int(D), int(page)))
 
 
@@ -609,6 +617,8 @@ def _cache_args(Hk, D, row_start, cached, table, page, cache):
     if row_start.numel() != B + 1 or cached.numel() != B:
         raise ValueError("table must be [B, pages of a sequence], row_start [B + 1] and cached [B]")
     size = sq_cache_page_bytes(Hk, D, page)
+    if not size:                                           # a refusal of the call's own, but for numbers that ctypes would cut to 32 bits
+        _int32(Hk=Hk, page=page)
     pages, rest = divmod(cache.numel(), size) if size else (0, 0)
     if rest:
         raise ValueError("cache is not a whole number of pages of sq_cache_page_bytes")
@@ -652,6 +662,10 @@ def sq_tree_attention(Q, row_start, cached, mask, table, page, cache, Hk, scale,
     lib = _lib or _load()
     T, Hq, D, ldq, ldo = _two_heads(Q, "Q", O, "O")
     B, per_sequence, pages = _cache_args(Hk, D, row_start, cached, table, page, cache)
+    if max_keys is None:
+        max_keys = min(per_sequence * page, 0x7FFFFFFF)
+    if max_rows > 0x7FFFFFFF or max_keys > 0x7FFFFFFF:
+        _int32(max_rows=max_rows, max_keys=max_keys)
     if mask is not None and (mask.dtype is not _i64 or not mask.is_contiguous() or mask.numel() != T):
         raise ValueError("mask must be int64, one word per row")
     if workspace is None:
@@ -662,8 +676,7 @@ def sq_tree_attention(Q, row_start, cached, mask, table, page, cache, Hk, scale,
         ws, ws_bytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
     code = lib.sq_tree_attention(
         Q.data_ptr(), ldq, T, Hq, Hk, D, row_start.data_ptr(), cached.data_ptr(), B, None if mask is None else mask.data_ptr(),
-        max_rows, per_sequence * page if max_keys is None else max_keys, table.data_ptr(), per_sequence, page, cache.data_ptr(),
-        pages, scale, O.data_ptr(), ldo, ws, ws_bytes,
+        max_rows, max_keys, table.data_ptr(), per_sequence, page, cache.data_ptr(), pages, scale, O.data_ptr(), ldo, ws, ws_bytes,
         _here(stream, Q, row_start, cached, table, cache, O, Q if mask is None else mask, Q if workspace is None else workspace))
     if code:
         _check(code)

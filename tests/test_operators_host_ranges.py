@@ -109,3 +109,21 @@ def test_library_loads_without_torch_names_of_its_own_gpu_build(lib, monkeypatch
     with pytest.raises(ValueError, match="device"):
         sq.sq_quantize_grouped(x, 32, torch.zeros(2, 32, dtype=torch.uint8), torch.zeros(2, 2, dtype=torch.float16))
     assert binding._raw_device is torch.cuda.current_device and callable(binding._raw_stream)
+
+
+def test_bindings_refuse_numbers_beyond_32_bits(lib):
+    """ctypes would pass on the lower 32 bits: 2^32 + 1 rows at most would be one."""
+    import torch
+    i = lambda *n: torch.zeros(n, dtype=torch.int32)        # noqa: E731
+    x, cache = torch.zeros(2, 3, 64, dtype=torch.float16), torch.zeros(4 * sq.sq_cache_page_bytes(3, 64, 16), dtype=torch.uint8)
+    def attention(**kw):
+        sq.sq_tree_attention(x, i(3), i(2), None, i(2, 2), kw.pop("page", 16), cache, kw.pop("Hk", 3), 0.1, x.clone(), **kw)
+    for bad in (dict(max_rows=2 ** 32 + 1), dict(max_keys=2 ** 32), dict(page=2 ** 32 + 16), dict(Hk=2 ** 32 + 3)):
+        with pytest.raises(ValueError, match="32 bits"):
+            attention(**bad)
+    with pytest.raises(ValueError, match="32 bits"):
+        sq.sq_cache_append(x, x, i(3), i(2), i(2, 2), 2 ** 32 + 16, cache)
+    assert sq.sq_cache_page_bytes(2 ** 32 + 3, 64, 16) == 0
+    for rot in (2 ** 32 + 64, 2 ** 40):
+        with pytest.raises(sq.SQError):
+            sq.sq_rotary_table(rot)
