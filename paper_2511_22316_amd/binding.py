@@ -515,7 +515,11 @@ def _here(stream, *tensors):
     for t in tensors:
         if t.get_device() != device:
             raise ValueError("tensors must be on the current device")
-    return _raw_stream(device) if stream is None else stream.cuda_stream
+    if stream is None:
+        return _raw_stream(device)
+    if getattr(stream, "device_index", device) != device:
+        raise ValueError("stream must be of the current device")
+    return stream.cuda_stream
 
 
 def sq_quantize_grouped(X, group, Q, steps, stream=None) -> None:

@@ -329,3 +329,22 @@ def test_a_sequence_that_begins_below_zero_is_left_out():
         for got in (k, v):
             assert np.array_equal(host(got)[own], want[own]) and (host(got)[~own] == 3.0).all()
         assert (host(o)[~own] == 3.0).all() and not (host(o)[own] == 3.0).all()
+
+
+def test_a_stream_of_another_device_is_refused():
+    """The work would be enqueued on a device that the tensors are not on."""
+    import types
+
+    import torch
+    import paper_2511_22316_amd as sq
+    print("case stream of another device", flush=True)
+    x = torch.ones(2, 64, dtype=torch.float16, device="cuda")
+    Q, steps = torch.zeros(2, 32, dtype=torch.uint8, device="cuda"), torch.zeros(2, 2, dtype=torch.float16, device="cuda")
+    own = torch.cuda.Stream()
+    other = types.SimpleNamespace(cuda_stream=own.cuda_stream, device_index=torch.cuda.current_device() + 1)
+    torch.cuda.synchronize()
+    with pytest.raises(ValueError, match="stream"):
+        sq.sq_quantize_grouped(x, 32, Q, steps, stream=other)
+    sq.sq_quantize_grouped(x, 32, Q, steps, stream=own)
+    torch.cuda.synchronize()
+    assert np.array_equal(host(Q), ou.pack(ou.quantize(np.ones((2, 2, 32)))[0].reshape(2, 64)))
