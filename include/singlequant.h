@@ -579,7 +579,8 @@ sq_status sq_cache_read(const void *cache, int32_t pages, int32_t Hk, int32_t D,
  *              shared out for the T rows there are; all sequences are split alike, so
  *              few rows over many keys are best not in one call with a long prompt.
  *   max_keys   about the longest cached[b] + new rows: how finely the work is split.
- *              Any value gives the right result.
+ *              Any value gives the right result; far above the lengths there are, most
+ *              splits have no keys, far below them a sequence is split less than it could be.
  *   scale      in (0, 1e20); scores scale * Q . k beyond 2^24 are not told apart
  *   workspace  device, 16-byte aligned, workspace_bytes long, or NULL and 0.  The sums
  *              of a split sequence meet in it; with less than

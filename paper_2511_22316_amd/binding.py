@@ -576,8 +576,9 @@ def sq_rotary_table(rot, base=10000.0, scaling=SQ_ROTARY_PLAIN, factor=1.0, trai
 
 
 def sq_rotary_fp16(X, positions, turns, half, Y, magnitude=1.0, stream=None) -> None:
-    """Rotary positions on X fp16 [T, H, D] (any token and head strides) -> Y of the same shape (may be X).  positions
-    int32 [T]; turns int64 [rot / 2] on the device, from sq_rotary_table; half: pairs (i, i + rot / 2), else (2i, 2i + 1)."""
+    """Rotary positions on X fp16 [T, H, D] -> Y of the same shape (may be X).  Heads and tokens may lie
+    apart, but a token's heads lie in front of the next token's (token stride >= (H - 1) head stride + D).  positions int32 [T];
+    turns int64 [rot / 2] on the device, from sq_rotary_table; half: pairs (i, i + rot / 2), else (2i, 2i + 1)."""
     lib = _lib or _load()
     shape = X.shape
     if Y.shape != shape:
@@ -662,7 +663,7 @@ def sq_tree_attention(Q, row_start, cached, mask, table, page, cache, Hk, scale,
                       stream=None) -> None:
     """Attention of the new rows Q fp16 [T, Hq, D] over the cache -> O [T, Hq, D].  mask int64 [T] (bit j: the row sees new
     row j of its sequence) or None (rows 0 .. i); max_rows: at least the new rows of every sequence; max_keys: about the
-    longest sequence (None: what the table holds); workspace: any contiguous device tensor, or None (nothing is split)."""
+    longest sequence (None: what the table holds, which splits long tables' short sequences badly); workspace: any contiguous device tensor, or None (nothing is split)."""
     lib = _lib or _load()
     T, Hq, D, ldq, ldo = _two_heads(Q, "Q", O, "O")
     B, per_sequence, pages = _cache_args(Hk, D, row_start, cached, table, page, cache)

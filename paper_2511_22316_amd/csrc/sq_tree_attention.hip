@@ -72,8 +72,9 @@ __device__ __forceinline__ int rows_of(const CacheView &c, const AttentionCall &
 }
 
 // The sequence with the place-th most keys (64 sequences at most; of more every one in its own place), so that the workgroups
-// of the longest start first: 16 trees of 31 to 61 rows and 2048 to 4096 keys 90 -> 84 us.  It costs a memory latency in front
-// of everything, so one row per sequence goes without (64 sequences of 512 to 1024 keys 21.4 us, 24.5 with it).
+// of the longest start first: 16 trees of 31 to 61 rows and 2048 to 4096 keys take 80 us, 87 in their own order.  It costs a memory latency
+// in front of everything (four prompts of 1024 to 2048 rows 168, 162 without), so one row per sequence goes without (64 sequences of 512
+// to 1024 keys took 3 us more with it).
 __device__ __forceinline__ int by_length(const CacheView &c, const AttentionCall &a, int place)
 {
     if (c.B == 1 || c.B > kWave) return place;
@@ -116,11 +117,11 @@ __device__ __forceinline__ int sequence_of_block(const CacheView &c, const Atten
 }
 
 // A workgroup takes one head of K and V of one sequence, 16 R query rows (row = new row * group + query head in the group)
-// and every splits-th chunk of its keys; its four waves take every fourth tile of 32 keys each and work alone until
-// the end.  What it does per key, whatever the rows, is most of the work of 16 of them (widening the codes: 120 of 260
-// instructions), so more rows are taken 32 at a time (R = 2) where there is enough to do: the trees above 116 -> 94 us, prompts of
-// 256 to 512 rows 189 -> 128.  Their query rows stay in LDS, so that three waves fit on a SIMD (four prompts of 2048 rows
-// 251 us with two, 225 so).  Neighbouring workgroups belong to an XCD and have a head of many sequences.
+// and every splits-th chunk of its keys (of max_keys / splits each, so one where max_keys tells the truth); its four waves take every
+// fourth tile of 32 keys each and work alone until the end.  What it does per key, whatever the rows, is most of the work of 16 of them (widening the codes: 120 of 260
+// instructions), so more rows are taken 32 at a time (R = 2) where there is enough to do: the trees above take 81 us, 90 with R = 1, four
+// prompts of 1024 to 2048 rows 169 and 189.  Their query rows stay in LDS, so that three waves fit on a SIMD (with two the prompts took
+// 12 % more).  Neighbouring workgroups belong to an XCD and have a head of many sequences.
 //
 // Scores: S^T = K Q^T on v_mfma_f32_16x16x32_f16, the keys as rows of the result and the query rows as columns, so a lane has
 // one query row (lane % 16) and four keys of each half of the tile (4 (lane / 16) + r); the weights it makes of them are
@@ -140,9 +141,9 @@ __device__ __forceinline__ int sequence_of_block(const CacheView &c, const Atten
 // every tile took 7% more); then it goes by the row's largest sum of a score and the logarithm of the step.  That logarithm is
 // the step's fp32 bits taken as a number, at most 0.09 too small, so the largest product then is 2^5.9 to 2^5.99: just below
 // a power of two, where the steps of fp16 are the finest for it and its followers, and 19 octaves above the subnormals,
-// whatever the values' steps are.  (16 trees / outputs' distance from their exact values in the 2-norm, where 2.1e-4 is the
-// rounding of the output: 2^7.9 83.5 us, 2.73e-4; 2^5.9 81.7, 2.81e-4; 2^1.9 79.8, 2.92e-4; 2^7 or 2^0 3.1e-4.  Two fp16 per
-// weight give 2.1e-4 and take 139 us instead of 117 with R = 1.)
+// whatever the values' steps are.  (The trees above / outputs' distance from their exact values in the 2-norm, where 2.1e-4 is the
+// rounding of the output: 2^7.9 83.7 us, 2.73e-4; 2^5.9 80.8, 2.81e-4; 2^1.9 2 % less again, 2.92e-4; 2^7 or 2^0 3.1e-4.  Two fp16 per
+// weight give 2.1e-4 and took a fifth more time with R = 1.)
 //
 // Loads: global memory -> LDS, two stages per wave; a tile goes to registers as soon as it has landed, and its stage is
 // requested again in front of the work on it, so two tiles are in flight all the time.  A wave waits for its own requests
@@ -166,7 +167,7 @@ __global__ __launch_bounds__(kWaves *kWave, D == 256 ? 2 : R == 2 ? 3 : 4) void 
     const int l16 = lane & 15, q = lane >> 4;
     if (PACKED && block_number() >= a.blocks) return;
     int id = PACKED ? xcd_contiguous_id((int)block_number(), a.blocks) : xcd_contiguous_id((int)blockIdx.x, (int)gridDim.x);
-    // of a prompt's rows the last ones see the most: they start first (4096 rows 221 -> 214 us; of a tree all see about the same)
+    // of a prompt's rows the last ones see the most: they start first (4096 rows 190 us, 199 in order; of a tree all see about the same)
     int row_block = a.mask ? id % a.row_blocks : a.row_blocks - 1 - id % a.row_blocks;
     id /= a.row_blocks;
     const int split = id % a.splits;
@@ -608,9 +609,10 @@ sq_status plan_tree_attention(int64_t T, int Hq, int Hk, int D, int B, int max_r
     auto packed = [&](int64_t per_block) { return T * group / per_block + B; };
     auto pack = [&](int64_t per_block) { return 2 * packed(per_block) < even(per_block) || even(per_block) * Hk > kGridRow; };
     auto row_blocks = [&](int64_t per_block) { return pack(per_block) ? packed(per_block) : even(per_block); };
-    // 32 rows per workgroup from about two waves of work for every SIMD on (us, 16 / 32: 16 sequences, 20 rows, 1024 keys 16.8 /
-    // 18.6; one prompt of 300 rows 13.2 / 15.3; 16 sequences, 32 rows, 4096 keys 30.5 / 30.7; one tree of 61 new rows, 16384 keys
-    // 44.7 / 39.9; 64 sequences, 28 rows, 8192 keys 122.7 / 103.2).  256 channels of two tiles of rows do not fit in registers.
+    // 32 rows per workgroup from about two waves of work for every SIMD on (us, 16 / 32, the same heads: 16 trees of 10 to 20 rows, 512 to
+    // 1024 keys 17.4 / 20.2; one prompt of 300 rows 8.9 / 11.2; one tree of 61 rows, 4096 keys 21.2 / 22.0, 16384 keys 45.6 / 39.0; 16 trees
+    // of 16 to 32 rows, 2048 to 4096 keys 55.7 / 49.4; 64 of 14 to 28 rows, 4096 to 8192 keys 265 / 250).  256 channels of two tiles
+    // of rows do not fit in registers.
     const int64_t per_block = D < 256 && rows > 16 && (double)(row_blocks(16) * Hk) * (double)max_keys > 0x1p20 ? 32 : 16;
     // Splits of the keys: as many as give every CU a workgroup, twice (four times, of many units) that while a split has 2048 keys
     // or more, no more than there are chunks of 128 keys, and none where the keys' tiles take less time than the second launch,

@@ -617,14 +617,20 @@ GroupedKernel choose_grouped_few(int64_t T, int K, int64_t N)
     return tiles == 1 || blocks * tiles <= 1024 ? kChannels64 : kChannels64Tokens32;
 }
 
-// Many tokens: the tile kernel of sq_w4a16_gemm with the steps on the widened codes.  Us per shape, groups of 128:
-//   64 x 128, two K groups    T = 333, K = N = 4096 26; 64 tokens in any case (K = 8192, N = 57344 108)
-//   128 x 128, two K groups   T = 333, K = N = 4096 33; T = 333, N = 9000 38.5 (64 x 128 45.6); T = 1000, N = 4096 44 (53)
-//   128 x 256                 T = 333, K = N = 4096 47; T = 600, N = 9000 56 (128 x 128 73); T = 64, K = 8192, N = 57344 120
-//   256 x 256                 1.85 times as long per round of 256 workgroups as 128 x 256, over seven shapes, so it is taken where
-//                             that is less: T = 4096, K = 11008, N = 4096 351 (389), T = 1500, K = 4096, N = 14336 218 (184)
-// T = 2048, K = N = 4096 takes 74.5 us with groups of 32 or 64 (sq_w4a16_gemm with its step per channel 65), T = 333, K = 5120,
-// N = 13824 69 (60): what the steps cost is the packed multiplication per two codes and power.
+// Many tokens: the tile kernel of sq_w4a16_gemm with the steps on the widened codes.  Us of one build with each shape, groups of 128, the
+// shape taken marked:
+//                            64 x 128   128 x 128   128 x 256   256 x 256
+//                               two K groups
+//   T = 333, K = N = 4096      28.7 *     35.4        47.6        88.8
+//   T = 333, N = 9000          48.7       40.0 *      51.7        90.8
+//   T = 1000, N = 4096         53.3       43.7 *      51.4        92.3
+//   T = 600, N = 9000          74.9       75.5        57.1 *      92.1
+//   T = 1500, N = 14336       248        228         184 *       213
+//   T = 4096, K = 11008       554        418         355         332 *
+//   T = 64, K = 8192, 57344   118 *      153         131         208          (64 tokens in any case)
+// 256 x 256 takes 1.85 times as long per round of 256 workgroups as 128 x 256 over such shapes, and is taken where that is less.
+// T = 2048, K = N = 4096 takes 72 to 76 us with groups of 32 to 128 (sq_w4a16_gemm with its step per channel 64 to 66), T = 333, K = 5120,
+// N = 13824 70 to 74 (63): what the steps cost is the packed multiplication per two codes and power.
 GroupedKernel choose_grouped_many(int64_t T, int K, int64_t N)
 {
     auto tiles = [&](int bm, int bn) { return (T + bm - 1) / bm * ((N + bn - 1) / bn); };

@@ -154,12 +154,13 @@ __device__ __forceinline__ void dma_step_if(const void *gptr, uint32_t lds_addr,
 // KG: groups of WM WN waves that walk K / KG elements each, through rings of their own, and add their sums through LDS.
 // GROUPED: a step per group of 1 << group_shift >= 32 elements of K in place of one per channel.  The step of a tile, or the
 // two of its halves, travel with it (a dword per channel; each is of another row, and their number is what these loads cost:
-// with a load per half T = 333, K = 5120, N = 13824, groups of 32 took 73.5 us, so 69.3), and a widened code is multiplied by its step in fp16, rounded once: a lane's 32
-// elements of a tile lie in one group, so that is one packed multiplication per two codes (four widening instructions
-// instead of three).  Scaling the sums instead would keep them exact, but wants as many registers again as the sums have.
-// Eight times a step from 8192 on is no fp16.  A wave notes the channels that have such steps on its way; where a workgroup has any it walks
-// over K once more (T = 2048, K = N = 4096: 75.7 us, 137 with such steps), those channels' codes taken by 1/8 and their sums by 8.  (Sums scaled in the middle of one walk: the
-// branch holds them twice, 60 registers more, and the large tiles spill.)
+// with a load per half T = 333, K = 5120, N = 13824, groups of 32 took 73.5 us, so 69.3), and a widened code is multiplied by its step
+// in fp16, rounded once: a lane's 32 elements of a tile lie in one group, so that is one packed multiplication per two codes (four
+// widening instructions instead of three).  Scaling the sums instead would keep them exact, but wants as many registers again as
+// the sums have.
+// Eight times a step from 8192 on is no fp16.  A wave notes the channels that have such steps on its way; where a workgroup has any it
+// walks over K once more (T = 2048, K = N = 4096: 75.7 us, 137 with such steps), those channels' codes taken by 1/8 and their sums by 8.
+// (Sums scaled in the middle of one walk: the branch holds them twice, 60 registers more, and the large tiles spill.)
 template <int WM, int WN, int FM, int FN, int OCC, int BK, int LW, int KG, bool GROUPED>
 __global__ __launch_bounds__((KG * WM * WN + LW) * kWave, OCC) void w4a16_gemm_ring_kernel(
     const __half *__restrict__ X, int64_t ldx, int T, int K, const uint8_t *__restrict__ Qw,
