@@ -348,3 +348,62 @@ def test_a_stream_of_another_device_is_refused():
     sq.sq_quantize_grouped(x, 32, Q, steps, stream=own)
     torch.cuda.synchronize()
     assert np.array_equal(host(Q), ou.pack(ou.quantize(np.ones((2, 2, 32)))[0].reshape(2, 64)))
+
+
+def test_ragged_batches_captured():
+    """A graph of a call whose row blocks are numbered by row_start, and whose sequences are split, replayed as the arrays' contents change:
+    which sequence has the prompt, how many rows there are, how long the cache is."""
+    import torch
+    import paper_2511_22316_amd as sq
+    print("case ragged captured", flush=True)
+    B, Hq, Hk, D, page, T = 12, 4, 1, 64, 16, 80            # T: the most rows of a step, those behind the last sequence padding
+    g = rng(44)
+    sets = []
+    for i in range(5):
+        new = [1] * B
+        new[(5 * i) % B], new[(5 * i + 3) % B] = 50 + 3 * i, i
+        past = list(g.integers(0, 40, B))
+        past[(5 * i) % B] = [3000, 10, 700, 0, 5000][i]
+        s = Setting(1700 + i, past, new, Hk, D, page)
+        Q = s.queries(Hq, 2.0)
+        sets.append((s, Q, *s.expect(Q, Hq // Hk, s.causal, 0.2)))
+    hint, workspace = 50000, 8 << 20
+    how = plan(T, Hq, Hk, D, B, 64, hint, workspace)
+    assert how[0] > 1 and how[2] == 1
+    per, pages = max(s.per for s, *_ in sets), max(s.cache.shape[0] for s, *_ in sets)
+    q, o = (torch.zeros(T, Hq, D, dtype=torch.float16, device="cuda") for _ in range(2))
+    start, cached, table = (torch.zeros(*n, dtype=torch.int32, device="cuda") for n in ((B + 1,), (B,), (B, per)))
+    cache = torch.zeros(pages, sets[0][0].size, dtype=torch.uint8, device="cuda")
+    ws = torch.empty(workspace, dtype=torch.uint8, device="cuda")
+
+    def load(s, Q):
+        q.zero_()
+        q[: s.T] = dev(Q)
+        o.fill_(3.0)
+        start.copy_(s.dstart)
+        cached.copy_(s.dcached)
+        table.fill_(-1)
+        table[:, : s.per] = s.dtable
+        cache[: s.cache.shape[0]] = s.cache
+        torch.cuda.synchronize()
+
+    def call():
+        sq.sq_tree_attention(q, start, cached, None, table, page, cache, Hk, 0.2, o, ws, max_rows=64, max_keys=hint)
+
+    load(*sets[0][:2])
+    call()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call()
+    for s, Q, want, bound in sets + sets[:2]:
+        load(s, Q)
+        graph.replay()
+        torch.cuda.synchronize()
+        replayed = o.clone()
+        ou.held(host(o[: s.T]), want, bound, "replayed")
+        assert (o[s.T:] == 3.0).all()
+        o.fill_(3.0)
+        call()
+        torch.cuda.synchronize()
+        assert torch.equal(o, replayed)
