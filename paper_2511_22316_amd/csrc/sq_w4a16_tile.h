@@ -390,8 +390,8 @@ __global__ __launch_bounds__((KG * WM * WN + LW) * kWave, OCC) void w4a16_gemm_r
             }
         }
         if constexpr (GROUPED) {
-            if (walk == 1) break;
             __syncthreads();                               // the flags are there, and all are done with the ring
+            if (walk == 1) break;
             uint32_t any = 0;
 #pragma unroll
             for (int k = 0; k < KG; ++k)
@@ -412,7 +412,7 @@ __global__ __launch_bounds__((KG * WM * WN + LW) * kWave, OCC) void w4a16_gemm_r
         constexpr int ACC = FM * FN * 16;
         static_assert((KG - 1) * NW * ACC * kWave * 4 <= KG * NS * STAGE, "the other groups' sums fit in the dead rings");
         float *sums = reinterpret_cast<float *>(ring) + wave * (ACC * kWave) + lane;
-        __syncthreads();
+        if constexpr (!GROUPED) __syncthreads();
         if (kg > 0) {
             float *mine = sums + (kg - 1) * (NW * ACC * kWave);
 #pragma unroll
